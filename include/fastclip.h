@@ -373,6 +373,140 @@ fastclip_status fastclip_check_indices(const int64_t* idx, int64_t b, int64_t N,
  * while epoch < decay_epochs, gamma_min afterwards.  Pure host function. */
 float fastclip_gamma_cosine(int64_t t, int64_t iters_per_epoch, int64_t decay_epochs, float gamma_min);
 
+/* ---- layers in front of the loss: layer norm, linear layers, AdamW ------------------------------------------------------
+ * The operators of the projection heads (and of the blocks of an encoder) whose outputs, normalised by
+ * fastclip_normalize_rows, are the rows of fastclip_step, and of the optimizer that takes their gradients.  The conventions
+ * are those above: device memory owned by the caller, no allocation, asynchronous on `stream`, host-checkable errors before
+ * anything is launched.  Matrices are row-major with a row stride in elements.  Outputs must not overlap inputs or each
+ * other.  Every sum is carried in fp32; an output is rounded once, to its storage type.  Results do not depend on timing: the
+ * same call on the same inputs gives the same bits.
+ *
+ * Layer norm over rows of width d:
+ *   mean = sum x / d,  rstd = 1 / sqrt(sum (x - mean)^2 / d + eps),  y = (x - mean) rstd weight + bias
+ * backward, with xh = (x - mean) rstd and q = dy weight:
+ *   dx = rstd (q - sum q / d - xh sum (q xh) / d),  dweight = sum over the rows of dy xh,  dbias = sum over the rows of dy */
+typedef struct {
+  uint32_t struct_size;      /* sizeof(fastclip_layer_norm_config) */
+  int32_t  x_dtype;          /* fastclip_dtype of x and dx */
+  int32_t  y_dtype;          /* fastclip_dtype of y and dy */
+  float    eps;              /* >= 0 */
+  int64_t  rows, d;          /* rows >= 0, d >= 1 */
+  int64_t  ld_x;             /* row stride of x and dx, >= d */
+  int64_t  ld_y;             /* row stride of y and dy, >= d */
+} fastclip_layer_norm_config;
+
+/* weight, bias [d] fp32, each NULL for one that is constant (1 and 0); mean, rstd [rows] fp32 out, each NULL to skip.
+ * Rows and strides of any size (rows, d and strides up to 2^31 - 1); 16-byte aligned rows of a multiple of 8 elements take the
+ * wide loads.  ERR_SHAPE: d < 1, rows < 0, a stride below d, struct_size; ERR_VALUE: a type, eps negative or not finite. */
+fastclip_status fastclip_layer_norm_forward(const fastclip_layer_norm_config* cfg, const void* x, const float* weight,
+                                            const float* bias, void* y, float* mean, float* rstd, void* stream);
+/* mean, rstd as the forward pass wrote them; weight NULL for ones.  dweight, dbias [d] fp32 out, overwritten, each NULL to
+ * skip.  workspace: fastclip_layer_norm_backward_workspace_bytes(cfg) bytes (0: invalid configuration), 256-byte aligned; its
+ * contents need no clearing. */
+size_t fastclip_layer_norm_backward_workspace_bytes(const fastclip_layer_norm_config* cfg);
+fastclip_status fastclip_layer_norm_backward(const fastclip_layer_norm_config* cfg, const void* x, const void* dy,
+                                             const float* mean, const float* rstd, const float* weight, void* dx,
+                                             float* dweight, float* dbias, void* workspace, size_t workspace_bytes,
+                                             void* stream);
+
+/* Linear layer of `rows` rows, d_in -> d_out, weights w [d_out, d_in]:
+ *   z = x w^T + bias,  y = act(z) + residual,  pre = z
+ * ACT_GELU: z Phi(z), Phi the normal distribution function; ACT_QUICK_GELU: z / (1 + exp(-1.702 z)).
+ * Storage: x, w, dy and pre in `dtype`; y, residual, dx and dw in `out_dtype`; bias and dbias fp32.  dtype BF16: products on
+ * the bf16 matrix cores, fp32 accumulation; dtype F32: products and sums in fp32 on the fp32 matrix cores. */
+typedef enum { FASTCLIP_ACT_NONE = 0, FASTCLIP_ACT_GELU = 1, FASTCLIP_ACT_QUICK_GELU = 2 } fastclip_activation;
+typedef enum {
+  FASTCLIP_LINEAR_FORWARD = 0, FASTCLIP_LINEAR_BACKWARD_INPUT = 1, FASTCLIP_LINEAR_BACKWARD_WEIGHT = 2
+} fastclip_linear_pass;
+
+typedef struct {
+  uint32_t struct_size;      /* sizeof(fastclip_linear_config) */
+  int32_t  dtype;            /* fastclip_dtype of x, w, dy, pre */
+  int32_t  out_dtype;        /* fastclip_dtype of y, residual, dx, dw */
+  int32_t  activation;       /* fastclip_activation */
+  int64_t  rows, d_in, d_out;   /* rows >= 0, widths >= 1 */
+  int64_t  ld_x;             /* row stride of x and dx, >= d_in */
+  int64_t  ld_w;             /* row stride of w and dw, >= d_in */
+  int64_t  ld_y;             /* row stride of y and dy, >= d_out */
+  int64_t  ld_pre;           /* row stride of pre: >= d_out in the forward pass (with pre), >= d_in in the backward pass of the
+                                input (with an activation) */
+  int64_t  ld_res;           /* row stride of residual, >= d_out (with residual) */
+} fastclip_linear_config;
+
+/* Bytes of workspace a pass needs (partial sums where its depth is split over workgroups; 0 if it needs none or the
+ * configuration is invalid).  256-byte aligned, contents need no clearing, NULL where 0. */
+size_t fastclip_linear_workspace_bytes(const fastclip_linear_config* cfg, int32_t pass);
+/* bias [d_out], residual [rows, ld_res] and pre [rows, ld_pre] (out) may each be NULL.
+ * dtype BF16: ERR_UNSUPPORTED if d_in, d_out or a row stride in use is no multiple of 8 or a matrix is not 16-byte aligned.  Any
+ * dtype: rows up to 2^30, widths and row strides up to 2^22, outputs up to what 2^23 tiles of 64 x 64 cover.  A row's sum that is infinite or NaN stays in its row and column. */
+fastclip_status fastclip_linear_forward(const fastclip_linear_config* cfg, const void* x, const void* w, const float* bias,
+                                        const void* residual, void* y, void* pre, void* workspace, size_t workspace_bytes,
+                                        void* stream);
+/* The gradient of a layer's input, times the derivative of the activation that made that input from `pre`:
+ *   dx = (dy w) act'(pre),  pre [rows, d_in];  activation NONE: pre is not read and may be NULL. */
+fastclip_status fastclip_linear_backward_input(const fastclip_linear_config* cfg, const void* dy, const void* w, const void* pre,
+                                               void* dx, void* workspace, size_t workspace_bytes, void* stream);
+/* dw = dy^T x [d_out, d_in], dbias = the sum of dy over the rows (NULL to skip); both overwritten (zeros for no rows).
+ * `activation` is not looked at. */
+fastclip_status fastclip_linear_backward_weight(const fastclip_linear_config* cfg, const void* dy, const void* x, void* dw,
+                                                float* dbias, void* workspace, size_t workspace_bytes, void* stream);
+
+/* AdamW over many tensors in one launch: for every element, with g its gradient and t = step,
+ *   m = beta1 m + (1 - beta1) g,  v = beta2 v + (1 - beta2) g^2,
+ *   p = p (1 - lr weight_decay) - lr (m / (1 - beta1^t)) / (sqrt(v / (1 - beta2^t)) + eps)
+ * and, where asked for, a bf16 copy of p for the next forward pass.
+ * state_bits 32: m, v fp32.  state_bits 8: a byte per element, blocks of 256 elements (from a tensor's first element on) share
+ * a power of two 2^k, held as the byte k + 127, k the exponent of the block's largest magnitude, -94 .. 126.  With f the exponent
+ * field and c the three bits behind the point, a code stands for
+ *   m: sign, 4-bit f, c:  +-(1 + c/8) 2^(f-14) 2^k,  f = 0: +-(c/8) 2^(-13) 2^k;
+ *   v: 5-bit f, c:          (1 + c/8) 2^(f-30) 2^k,  f = 0:   (c/8) 2^(-29) 2^k.
+ * p moves by the unrounded moments; these are formed in fp64 (a rounding decides which code is stored) and rounded to a code up
+ * or down with the probability of the remainder: up if remainder + r / 2^16 >= 1, r 16 bits of a hash of (seed, tensor number,
+ * element) (the low half for m, the high half for v), so that a moment that moves by less than a step still moves on average.
+ * A positive v is never stored as zero.  Moments that are not finite are stored as the largest code (p itself becomes NaN). */
+typedef struct {
+  uint32_t struct_size;      /* sizeof(fastclip_adamw_config) */
+  int32_t  state_bits;       /* 32 or 8 */
+  int32_t  grad_dtype;       /* fastclip_dtype of every gradient */
+  uint32_t seed;             /* 8-bit states: another one every step */
+  int64_t  step;             /* t >= 1 */
+  float    lr, beta1, beta2, eps;   /* finite, lr >= 0, 0 <= beta < 1, eps >= 0 */
+} fastclip_adamw_config;
+
+typedef struct {             /* DEVICE memory; param, m, v and the exponents are updated in place */
+  float*      param;         /* [n] */
+  const void* grad;          /* [n] grad_dtype */
+  void*       m;             /* [n] fp32 or bytes */
+  void*       v;             /* [n] */
+  void*       param_bf16;    /* [n] out, NULL to skip */
+  uint8_t*    m_exp;         /* [ceil(n / 256)] with 8 bits, else not looked at */
+  uint8_t*    v_exp;
+  int64_t     n;             /* >= 0 */
+  float       weight_decay;  /* finite, >= 0 */
+  int32_t     reserved;      /* 0 */
+} fastclip_adamw_tensor;
+
+/* The table of tensors, made once and kept in device memory by the caller: fill writes fastclip_adamw_table_bytes() bytes of
+ * HOST memory, which the caller copies to the device (256-byte aligned), and *table, whose `device` the caller sets.  It holds
+ * addresses: the tensors stay where they are as long as it is in use.  Pure host functions.  Pointers have the natural alignment
+ * of their types (16-byte aligned tensors take the wide loads). */
+typedef struct {
+  uint32_t struct_size;      /* sizeof(fastclip_adamw_table) */
+  int32_t  state_bits, grad_dtype;   /* what it was made for */
+  int32_t  reserved;
+  int64_t  tensors, chunks;
+  const void* device;        /* the table in device memory */
+} fastclip_adamw_table;
+size_t fastclip_adamw_table_bytes(const fastclip_adamw_tensor* tensors, int64_t count);
+fastclip_status fastclip_adamw_table_fill(const fastclip_adamw_config* cfg, const fastclip_adamw_tensor* tensors, int64_t count,
+                                          void* host_table, size_t bytes, fastclip_adamw_table* table);
+/* ERR_VALUE: *table was made for other state_bits or another gradient type. */
+fastclip_status fastclip_adamw_step(const fastclip_adamw_config* cfg, const fastclip_adamw_table* table, void* stream);
+/* The values that n elements of an 8-bit moment stand for, out [n] fp32: for checkpoints and for tests. */
+typedef enum { FASTCLIP_ADAMW_FIRST = 1, FASTCLIP_ADAMW_SECOND = 2 } fastclip_adamw_moment;
+fastclip_status fastclip_adamw_state_values(int32_t moment, const uint8_t* codes, const uint8_t* exponents, int64_t n,
+                                            float* out, void* stream);
+
 const char* fastclip_status_string(fastclip_status s);
 
 /* Text of the HIP error behind the most recent FASTCLIP_ERR_LAUNCH on the calling thread

@@ -62,6 +62,39 @@ class fastclip_tau_state(C.Structure):
     _fields_ = [(n, C.c_void_p) for n in _TAU_STATE_FIELDS]
 
 
+ACT_NONE, ACT_GELU, ACT_QUICK_GELU = 0, 1, 2
+LINEAR_FORWARD, LINEAR_BACKWARD_INPUT, LINEAR_BACKWARD_WEIGHT = 0, 1, 2
+ADAMW_FIRST, ADAMW_SECOND = 1, 2
+ADAMW_BLOCK = 256           # elements of an 8-bit moment that share an exponent
+
+
+class fastclip_layer_norm_config(C.Structure):
+    _fields_ = [("struct_size", C.c_uint32), ("x_dtype", C.c_int32), ("y_dtype", C.c_int32), ("eps", C.c_float),
+                ("rows", C.c_int64), ("d", C.c_int64), ("ld_x", C.c_int64), ("ld_y", C.c_int64)]
+
+
+class fastclip_linear_config(C.Structure):
+    _fields_ = [("struct_size", C.c_uint32), ("dtype", C.c_int32), ("out_dtype", C.c_int32), ("activation", C.c_int32),
+                ("rows", C.c_int64), ("d_in", C.c_int64), ("d_out", C.c_int64), ("ld_x", C.c_int64), ("ld_w", C.c_int64),
+                ("ld_y", C.c_int64), ("ld_pre", C.c_int64), ("ld_res", C.c_int64)]
+
+
+class fastclip_adamw_config(C.Structure):
+    _fields_ = [("struct_size", C.c_uint32), ("state_bits", C.c_int32), ("grad_dtype", C.c_int32), ("seed", C.c_uint32),
+                ("step", C.c_int64), ("lr", C.c_float), ("beta1", C.c_float), ("beta2", C.c_float), ("eps", C.c_float)]
+
+
+class fastclip_adamw_tensor(C.Structure):
+    _fields_ = [("param", C.c_void_p), ("grad", C.c_void_p), ("m", C.c_void_p), ("v", C.c_void_p),
+                ("param_bf16", C.c_void_p), ("m_exp", C.c_void_p), ("v_exp", C.c_void_p), ("n", C.c_int64),
+                ("weight_decay", C.c_float), ("reserved", C.c_int32)]
+
+
+class fastclip_adamw_table(C.Structure):
+    _fields_ = [("struct_size", C.c_uint32), ("state_bits", C.c_int32), ("grad_dtype", C.c_int32), ("reserved", C.c_int32),
+                ("tensors", C.c_int64), ("chunks", C.c_int64), ("device", C.c_void_p)]
+
+
 _lib = None
 
 
@@ -128,6 +161,30 @@ def load(build_if_missing: bool = True):
     lib.fastclip_measure_strips.restype = C.c_int
     lib.fastclip_measure_strips.argtypes = [cfgp, bufp, C.c_void_p, C.c_size_t, C.c_void_p, C.c_int32, C.c_int32,
                                             C.POINTER(C.c_float), C.POINTER(C.c_double)]
+    lnp, linp = C.POINTER(fastclip_layer_norm_config), C.POINTER(fastclip_linear_config)
+    adcp, adtp, adbp = C.POINTER(fastclip_adamw_config), C.POINTER(fastclip_adamw_tensor), C.POINTER(fastclip_adamw_table)
+    lib.fastclip_layer_norm_forward.restype = C.c_int
+    lib.fastclip_layer_norm_forward.argtypes = [lnp] + [C.c_void_p] * 7
+    lib.fastclip_layer_norm_backward_workspace_bytes.restype = C.c_size_t
+    lib.fastclip_layer_norm_backward_workspace_bytes.argtypes = [lnp]
+    lib.fastclip_layer_norm_backward.restype = C.c_int
+    lib.fastclip_layer_norm_backward.argtypes = [lnp] + [C.c_void_p] * 9 + [C.c_size_t, C.c_void_p]
+    lib.fastclip_linear_workspace_bytes.restype = C.c_size_t
+    lib.fastclip_linear_workspace_bytes.argtypes = [linp, C.c_int32]
+    lib.fastclip_linear_forward.restype = C.c_int
+    lib.fastclip_linear_forward.argtypes = [linp] + [C.c_void_p] * 7 + [C.c_size_t, C.c_void_p]
+    lib.fastclip_linear_backward_input.restype = C.c_int
+    lib.fastclip_linear_backward_input.argtypes = [linp] + [C.c_void_p] * 5 + [C.c_size_t, C.c_void_p]
+    lib.fastclip_linear_backward_weight.restype = C.c_int
+    lib.fastclip_linear_backward_weight.argtypes = [linp] + [C.c_void_p] * 5 + [C.c_size_t, C.c_void_p]
+    lib.fastclip_adamw_table_bytes.restype = C.c_size_t
+    lib.fastclip_adamw_table_bytes.argtypes = [adtp, C.c_int64]
+    lib.fastclip_adamw_table_fill.restype = C.c_int
+    lib.fastclip_adamw_table_fill.argtypes = [adcp, adtp, C.c_int64, C.c_void_p, C.c_size_t, adbp]
+    lib.fastclip_adamw_step.restype = C.c_int
+    lib.fastclip_adamw_step.argtypes = [adcp, adbp, C.c_void_p]
+    lib.fastclip_adamw_state_values.restype = C.c_int
+    lib.fastclip_adamw_state_values.argtypes = [C.c_int32, C.c_void_p, C.c_void_p, C.c_int64, C.c_void_p, C.c_void_p]
     lib.fastclip_last_hip_error.restype = C.c_char_p
     lib.fastclip_last_hip_error.argtypes = []
     _lib = lib
@@ -368,6 +425,146 @@ def fastclip_check_indices(idx, b, N, workspace, workspace_bytes=None, stream=No
 
 def fastclip_gamma_cosine(t, iters_per_epoch, decay_epochs, gamma_min) -> float:
     return float(load().fastclip_gamma_cosine(int(t), int(iters_per_epoch), int(decay_epochs), float(gamma_min)))
+
+
+# ---- layers in front of the loss -----------------------------------------------------------------------------------
+
+def make_layer_norm_config(*, rows, d, x_dtype, y_dtype, eps, ld_x=None, ld_y=None) -> fastclip_layer_norm_config:
+    return fastclip_layer_norm_config(C.sizeof(fastclip_layer_norm_config), int(x_dtype), int(y_dtype), float(eps), int(rows),
+                                      int(d), int(d if ld_x is None else ld_x), int(d if ld_y is None else ld_y))
+
+
+def fastclip_layer_norm_forward(cfg, x, weight, bias, y, mean=None, rstd=None, stream=None, check=True) -> int:
+    """weight, bias, mean, rstd: None for ones, zeros, not wanted."""
+    st = int(load().fastclip_layer_norm_forward(C.byref(cfg), _ptr(x), _ptr(weight), _ptr(bias), _ptr(y), _ptr(mean),
+                                                _ptr(rstd), _stream(stream)))
+    if check and st != OK:
+        raise FastclipError(st)
+    return st
+
+
+def fastclip_layer_norm_backward_workspace_bytes(cfg) -> int:
+    return int(load().fastclip_layer_norm_backward_workspace_bytes(C.byref(cfg)))
+
+
+def _nbytes(workspace, workspace_bytes):
+    if workspace_bytes is not None:
+        return workspace_bytes
+    return 0 if workspace is None else workspace.numel() * workspace.element_size()
+
+
+def fastclip_layer_norm_backward(cfg, x, dy, mean, rstd, weight, dx, dweight, dbias, workspace, workspace_bytes=None,
+                                 stream=None, check=True) -> int:
+    """dweight, dbias: None where not wanted; workspace: CUDA uint8 tensor (or raw address with workspace_bytes given)."""
+    st = int(load().fastclip_layer_norm_backward(C.byref(cfg), _ptr(x), _ptr(dy), _ptr(mean), _ptr(rstd), _ptr(weight), _ptr(dx),
+                                                 _ptr(dweight), _ptr(dbias), _ptr(workspace),
+                                                 _nbytes(workspace, workspace_bytes), _stream(stream)))
+    if check and st != OK:
+        raise FastclipError(st)
+    return st
+
+
+def make_linear_config(*, rows, d_in, d_out, dtype, out_dtype=None, activation=ACT_NONE, ld_x=None, ld_w=None, ld_y=None,
+                       ld_pre=None, ld_res=None) -> fastclip_linear_config:
+    """Strides default to dense rows; ld_pre to that of the forward pass (d_out)."""
+    pick = lambda ld, d: int(d if ld is None else ld)
+    return fastclip_linear_config(C.sizeof(fastclip_linear_config), int(dtype), int(dtype if out_dtype is None else out_dtype),
+                                  int(activation), int(rows), int(d_in), int(d_out), pick(ld_x, d_in), pick(ld_w, d_in),
+                                  pick(ld_y, d_out), pick(ld_pre, d_out), pick(ld_res, d_out))
+
+
+def fastclip_linear_workspace_bytes(cfg, linear_pass) -> int:
+    return int(load().fastclip_linear_workspace_bytes(C.byref(cfg), int(linear_pass)))
+
+
+def fastclip_linear_forward(cfg, x, w, bias, residual, y, pre=None, workspace=None, workspace_bytes=None, stream=None,
+                            check=True) -> int:
+    st = int(load().fastclip_linear_forward(C.byref(cfg), _ptr(x), _ptr(w), _ptr(bias), _ptr(residual), _ptr(y), _ptr(pre),
+                                            _ptr(workspace), _nbytes(workspace, workspace_bytes), _stream(stream)))
+    if check and st != OK:
+        raise FastclipError(st)
+    return st
+
+
+def fastclip_linear_backward_input(cfg, dy, w, pre, dx, workspace=None, workspace_bytes=None, stream=None, check=True) -> int:
+    st = int(load().fastclip_linear_backward_input(C.byref(cfg), _ptr(dy), _ptr(w), _ptr(pre), _ptr(dx), _ptr(workspace),
+                                                   _nbytes(workspace, workspace_bytes), _stream(stream)))
+    if check and st != OK:
+        raise FastclipError(st)
+    return st
+
+
+def fastclip_linear_backward_weight(cfg, dy, x, dw, dbias=None, workspace=None, workspace_bytes=None, stream=None,
+                                    check=True) -> int:
+    st = int(load().fastclip_linear_backward_weight(C.byref(cfg), _ptr(dy), _ptr(x), _ptr(dw), _ptr(dbias), _ptr(workspace),
+                                                    _nbytes(workspace, workspace_bytes), _stream(stream)))
+    if check and st != OK:
+        raise FastclipError(st)
+    return st
+
+
+def make_adamw_config(*, state_bits, grad_dtype, step, lr, beta1, beta2, eps=1e-8, seed=0) -> fastclip_adamw_config:
+    return fastclip_adamw_config(C.sizeof(fastclip_adamw_config), int(state_bits), int(grad_dtype), int(seed) & 0xFFFFFFFF,
+                                 int(step), float(lr), float(beta1), float(beta2), float(eps))
+
+
+def make_adamw_tensor(*, param, grad, m, v, param_bf16=None, weight_decay=0.0, m_exp=None, v_exp=None) -> fastclip_adamw_tensor:
+    """Contiguous CUDA tensors of one size: param fp32, grad fp32 or bf16, m and v fp32 or uint8 (then with the blocks'
+    exponents).  The struct keeps them referenced."""
+    n = param.numel()
+    held = [t for t in (param, grad, m, v, param_bf16, m_exp, v_exp) if t is not None]
+    if not all(t.is_contiguous() for t in held):
+        raise ValueError("adamw tensors must be contiguous")
+    if any(t is not None and t.numel() != n for t in (grad, m, v, param_bf16)):
+        raise ValueError("param, grad, m, v and param_bf16 must have the same number of elements")
+    if any(t is not None and t.numel() != -(-n // ADAMW_BLOCK) for t in (m_exp, v_exp)):
+        raise ValueError("an exponent for every block of %d elements" % ADAMW_BLOCK)
+    out = fastclip_adamw_tensor(_ptr(param), _ptr(grad), _ptr(m), _ptr(v), _ptr(param_bf16), _ptr(m_exp), _ptr(v_exp), n,
+                                float(weight_decay), 0)
+    out._keepalive = held
+    out._types = tuple(None if t is None else str(t.dtype) for t in (param, grad, m, v, param_bf16, m_exp, v_exp))
+    return out
+
+
+def make_adamw_table(cfg, tensors) -> fastclip_adamw_table:
+    """The device table of a list of make_adamw_tensor()s, for every later step on them; keeps them referenced."""
+    import torch
+    grad = {BF16: "torch.bfloat16", F32: "torch.float32"}.get(cfg.grad_dtype)
+    state, exps = ("torch.uint8", "torch.uint8") if cfg.state_bits == 8 else ("torch.float32", None)
+    for t in tensors:
+        want = ("torch.float32", grad, state, state, "torch.bfloat16", exps, exps)
+        for have, wanted, optional in zip(t._types, want, (False, False, False, False, True, False, False)):
+            if wanted is not None and have != wanted and not (optional and have is None):
+                raise TypeError("adamw tensor of type %s where %s is wanted" % (have, wanted))
+    lib, n = load(), len(tensors)
+    array = (fastclip_adamw_tensor * max(1, n))(*tensors)
+    nbytes = int(lib.fastclip_adamw_table_bytes(array, n))
+    host = torch.zeros(max(1, nbytes), dtype=torch.uint8)
+    table = fastclip_adamw_table()
+    st = int(lib.fastclip_adamw_table_fill(C.byref(cfg), array, n, host.data_ptr(), nbytes, C.byref(table)))
+    if st != OK:
+        raise FastclipError(st)
+    device = next((k.device for t in tensors for k in t._keepalive), None)
+    if device is not None and table.chunks:
+        room = host.to(device)                 # from pageable memory: complete when the call returns
+        table.device = room.data_ptr()
+        table._keepalive = (room, [t._keepalive for t in tensors])
+    return table
+
+
+def fastclip_adamw_step(cfg, table, stream=None, check=True) -> int:
+    st = int(load().fastclip_adamw_step(C.byref(cfg), C.byref(table), _stream(stream)))
+    if check and st != OK:
+        raise FastclipError(st)
+    return st
+
+
+def fastclip_adamw_state_values(moment, codes, exponents, n, out, stream=None, check=True) -> int:
+    st = int(load().fastclip_adamw_state_values(int(moment), _ptr(codes), _ptr(exponents), int(n), _ptr(out),
+                                                _stream(stream)))
+    if check and st != OK:
+        raise FastclipError(st)
+    return st
 
 
 def fastclip_last_hip_error() -> str:

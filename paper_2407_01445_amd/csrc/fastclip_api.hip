@@ -15,7 +15,7 @@ static bool bad_float(float x) { return !(x == x) || isinf(x); }
 
 static thread_local hipError_t g_last_hip_error = hipSuccess;
 // Reads and clears the runtime's error state; remembers a failure for fastclip_last_hip_error.
-static fastclip_status launch_status() {
+fastclip_status launch_status() {
   const hipError_t e = hipGetLastError();
   if (e == hipSuccess) return FASTCLIP_OK;
   g_last_hip_error = e;

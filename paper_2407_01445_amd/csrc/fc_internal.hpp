@@ -111,6 +111,7 @@ static inline int strips_t128_anchors(const Layout& L) {
 // Waves of k_contract_t128_bf16 that finish the anchors of an output tile where no workgroup of its own does.
 static inline int t128_finishing_waves(int out_rows) { return out_rows == 32 ? 2 : out_rows / 32; }
 
+fastclip_status launch_status();   // what the launches since the last call came to; remembers a failure
 fastclip_status validate(const fastclip_config* cfg, const fastclip_buffers* bufs);
 void make_layout(const fastclip_config& cfg, Layout* L);
 

@@ -1,0 +1,306 @@
+// AdamW over a table of tensors in one launch, moments in fp32 or in 8 bits (gfx950, wave64).
+//
+//   m = b1 m + (1 - b1) g,  v = b2 v + (1 - b2) g^2,  p = p (1 - lr wd) - lr/(1 - b1^t) m / (sqrt(v / (1 - b2^t)) + eps)
+//
+// Bound by memory: 26 bytes an element with bf16 gradients (30 with fp32 moments written out and the bf16 copy), nothing is
+// used twice.  A workgroup takes a chunk of 4096 elements of one tensor, 16 a thread; all of a thread's loads are requested
+// before the first is used.  The table says which chunk of which tensor a workgroup has, so that 180 small and large tensors
+// are one launch without a search.
+#include "operators.hpp"
+
+namespace fc {
+
+typedef __attribute__((__vector_size__(4 * sizeof(uint32_t)))) uint32_t u32x4;
+typedef __attribute__((__vector_size__(2 * sizeof(uint32_t)))) uint32_t u32x2;
+
+__device__ __forceinline__ uint32_t adamw_bf16(float x) { return __builtin_bit_cast(uint16_t, (__bf16)x); }
+
+struct AdamwScalars {
+  float beta1, beta2, rest1, rest2, step_size, corr2, eps, decay;   // rest = 1 - beta, decay = lr weight_decay
+};
+__device__ __forceinline__ AdamwScalars adamw_scalars(const AdamwArgs& a, float weight_decay) {
+  return {a.beta1, a.beta2, 1.f - a.beta1, 1.f - a.beta2, a.step_size, a.corr2, a.eps, a.lr * weight_decay};
+}
+__device__ __forceinline__ float adamw_move(float p, float m, float v, const AdamwScalars& k) {
+  return p - fmaf(p, k.decay, (m * k.step_size) / (sqrtf(v * k.corr2) + k.eps));
+}
+// b1 m + (1 - b1) g with one rounding of the sum and none of its terms: where they cancel, the first moment is all there is of p's
+// step, and two more instructions do not show beside the memory traffic
+__device__ __forceinline__ float adamw_first(float m, float g, const AdamwScalars& k) {
+  const float t = g * k.rest1;
+  return fmaf(m, k.beta1, t) + fmaf(g, k.rest1, -t);
+}
+
+// four elements as they lie in memory: gradients
+template <bool BF16>
+struct Grad4 {
+  u32x4 w;
+  __device__ void load(const void* g, int64_t i) { w = *(const u32x4*)((const float*)g + i); }
+  __device__ float get(int i) const { return __uint_as_float(w[i]); }
+};
+template <>
+struct Grad4<true> {
+  u32x2 w;
+  __device__ void load(const void* g, int64_t i) { w = *(const u32x2*)((const bf16_t*)g + i); }
+  __device__ float get(int i) const { return __uint_as_float(i & 1 ? w[i >> 1] & 0xffff0000u : w[i >> 1] << 16); }
+};
+template <bool BF16>
+__device__ __forceinline__ float grad_at(const void* g, int64_t i) {
+  return BF16 ? __uint_as_float((uint32_t)((const bf16_t*)g)[i] << 16) : ((const float*)g)[i];
+}
+
+template <bool BF16>
+__global__ void __launch_bounds__(256) k_adamw_32(AdamwArgs a) {
+  const AdamwChunk where = a.chunks[blockIdx.x];
+  const AdamwEntry& e = a.entries[where.tensor];
+  const int64_t first = (int64_t)where.chunk * kAdamwChunk, n = e.n;
+  const AdamwScalars k = adamw_scalars(a, e.weight_decay);
+  float* __restrict__ p = e.param;
+  float* __restrict__ m = (float*)e.m;
+  float* __restrict__ v = (float*)e.v;
+  const void* __restrict__ g = e.grad;
+  uint16_t* __restrict__ copy = e.copy;
+  if (e.wide && first + kAdamwChunk <= n) {
+    float4 p4[4], m4[4], v4[4];
+    Grad4<BF16> g4[4];
+#pragma unroll
+    for (int j = 0; j < 4; ++j) {
+      const int64_t i = first + j * 1024 + threadIdx.x * 4;
+      p4[j] = *(const float4*)(p + i);
+      m4[j] = *(const float4*)(m + i);
+      v4[j] = *(const float4*)(v + i);
+      g4[j].load(g, i);
+    }
+#pragma unroll
+    for (int j = 0; j < 4; ++j) {
+      const int64_t i = first + j * 1024 + threadIdx.x * 4;
+      float pe[4] = {p4[j].x, p4[j].y, p4[j].z, p4[j].w}, me[4] = {m4[j].x, m4[j].y, m4[j].z, m4[j].w},
+            ve[4] = {v4[j].x, v4[j].y, v4[j].z, v4[j].w};
+#pragma unroll
+      for (int q = 0; q < 4; ++q) {
+        const float x = g4[j].get(q);
+        me[q] = adamw_first(me[q], x, k);
+        ve[q] = fmaf(ve[q], k.beta2, x * x * k.rest2);
+        pe[q] = adamw_move(pe[q], me[q], ve[q], k);
+      }
+      *(float4*)(p + i) = make_float4(pe[0], pe[1], pe[2], pe[3]);
+      *(float4*)(m + i) = make_float4(me[0], me[1], me[2], me[3]);
+      *(float4*)(v + i) = make_float4(ve[0], ve[1], ve[2], ve[3]);
+      if (copy) {
+        const u32x2 c = {adamw_bf16(pe[0]) | adamw_bf16(pe[1]) << 16, adamw_bf16(pe[2]) | adamw_bf16(pe[3]) << 16};
+        *(u32x2*)(copy + i) = c;
+      }
+    }
+    return;
+  }
+  const int64_t end = first + kAdamwChunk < n ? first + kAdamwChunk : n;
+  for (int64_t i = first + threadIdx.x; i < end; i += 256) {
+    const float x = grad_at<BF16>(g, i);
+    const float me = adamw_first(m[i], x, k), ve = fmaf(v[i], k.beta2, x * x * k.rest2);
+    const float pe = adamw_move(p[i], me, ve, k);
+    p[i] = pe;
+    m[i] = me;
+    v[i] = ve;
+    if (copy) copy[i] = (uint16_t)adamw_bf16(pe);
+  }
+}
+
+// ---- moments in 8 bits ---------------------------------------------------------------------------------------------------
+//
+// A code of F exponent bits and three bits c behind the point, taken as the exponent and the first three mantissa bits of an
+// fp32 number (code << 20), is that number over 2^(127 - F'), F' = 14 for m, 30 for v - zero exponents too, which are fp32's
+// denormals.  So a value is one exact fp64 product with 2^(127 - F') 2^k, and the factor beta goes into the same constant.
+//
+// A new value x of a block of exponent k, in [0, 2^(k + 1)), has to become floor(|x| 2^(3 + F' - k - f) + r / 2^16) on top of
+// (f - 1) 8, f = max(1, exponent of x - k + F').  Only the first 20 bits of |x| 2^(19 + F' - k - f) matter for the integer part of
+// that times 2^16, and they are in the upper half of the fp64 number: its 21 bits, shifted right by 1, or further where f = 1
+// already.  The fp64 moments decide which code it is; everything behind them is 32-bit integers.
+constexpr int kFirstTop = 14, kSecondTop = 30;
+
+__device__ __forceinline__ uint32_t adamw_mix(uint32_t x) {
+  x ^= x >> 16;
+  x *= 0x6A09E667u;
+  x ^= x >> 15;
+  x *= 0xBB67AE85u;
+  return x ^ (x >> 16);
+}
+__device__ __forceinline__ uint32_t upper_half(double x) { return (uint32_t)(__builtin_bit_cast(uint64_t, x) >> 32); }
+// 2^e for -1022 <= e <= 1023
+__device__ __forceinline__ double pow2(int e) { return __builtin_bit_cast(double, (uint64_t)(e + 1023) << 52); }
+
+// hi: upper half of |x|; k1: the block's exponent + 1023
+template <int TOP>
+__device__ __forceinline__ uint32_t adamw_code(uint32_t hi, int k1, uint32_t r16) {
+  const int field = (int)(hi >> 20) - k1 + TOP;
+  const int shift = field >= 1 ? 1 : (field > -30 ? 2 - field : 31);
+  const uint32_t mantissa = (hi & 0xFFFFFu) | 0x100000u;
+  const uint32_t q = ((mantissa >> shift) + r16) >> 16;
+  const uint32_t code = (field >= 1 ? (uint32_t)(field - 1) * 8u : 0u) + q;
+  const uint32_t most = TOP == kFirstTop ? 127u : 255u;
+  return code < most ? code : most;
+}
+__device__ __forceinline__ int block_exponent(uint32_t hi) {      // of a block's largest magnitude
+  const int k = (int)(hi >> 20) - 1023;
+  return k < -94 ? -94 : (k > 126 ? 126 : k);
+}
+__device__ __forceinline__ uint32_t larger(uint32_t x, uint32_t y) { return x > y ? x : y; }
+__device__ __forceinline__ uint32_t wave_largest(uint32_t x) {
+#pragma unroll
+  for (int s = 32; s > 0; s >>= 1) x = larger(x, __shfl_xor(x, s));
+  return x;
+}
+
+// A wavefront takes a block, four elements a lane.
+template <bool BF16>
+__global__ void __launch_bounds__(256) k_adamw_8(AdamwArgs a) {
+  const AdamwChunk where = a.chunks[blockIdx.x];
+  const AdamwEntry& e = a.entries[where.tensor];
+  const int64_t n = e.n;
+  const AdamwScalars k = adamw_scalars(a, e.weight_decay);
+  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+  float* __restrict__ p = e.param;
+  uint8_t* __restrict__ m = (uint8_t*)e.m;
+  uint8_t* __restrict__ v = (uint8_t*)e.v;
+  const void* __restrict__ g = e.grad;
+  uint16_t* __restrict__ copy = e.copy;
+  const uint32_t key = adamw_mix(a.seed + 0x9E3779B9u * (uint32_t)(where.tensor + 1));
+  const double b1 = (double)a.beta1, b2 = (double)a.beta2, c1 = 1.0 - b1, c2 = 1.0 - b2;
+  const bool wide = e.wide != 0;
+  float4 p4[4];
+  Grad4<BF16> g4[4];
+  uint32_t mw[4], vw[4];
+  int em[4], ev[4];
+  const int64_t block0 = (int64_t)where.chunk * (kAdamwChunk / kAdamwBlock) + wave;     // this wavefront's: block0 + 4 j
+#pragma unroll
+  for (int j = 0; j < 4; ++j) {
+    const int64_t block = block0 + 4 * j, i = block * kAdamwBlock + 4 * lane;
+    if (block * kAdamwBlock >= n) continue;      // the whole wavefront
+    em[j] = e.m_exp[block];
+    ev[j] = e.v_exp[block];
+    if (wide && (block + 1) * kAdamwBlock <= n) {
+      p4[j] = *(const float4*)(p + i);
+      g4[j].load(g, i);
+      mw[j] = *(const uint32_t*)(m + i);
+      vw[j] = *(const uint32_t*)(v + i);
+    }
+  }
+#pragma unroll
+  for (int j = 0; j < 4; ++j) {
+    const int64_t block = block0 + 4 * j, i = block * kAdamwBlock + 4 * lane;
+    if (block * kAdamwBlock >= n) continue;
+    const bool whole = wide && (block + 1) * kAdamwBlock <= n;
+    float pe[4], ge[4];
+    uint32_t mc = mw[j], vc = vw[j];
+    if (whole) {
+      pe[0] = p4[j].x; pe[1] = p4[j].y; pe[2] = p4[j].z; pe[3] = p4[j].w;
+#pragma unroll
+      for (int q = 0; q < 4; ++q) ge[q] = g4[j].get(q);
+    } else {
+      mc = vc = 0;
+#pragma unroll
+      for (int q = 0; q < 4; ++q) {
+        const bool in = i + q < n;
+        pe[q] = in ? p[i + q] : 0.f;
+        ge[q] = in ? grad_at<BF16>(g, i + q) : 0.f;
+        mc |= (in ? (uint32_t)m[i + q] : 0u) << (8 * q);
+        vc |= (in ? (uint32_t)v[i + q] : 0u) << (8 * q);
+      }
+    }
+    const double fm = b1 * pow2(127 - kFirstTop + em[j] - 127), fv = b2 * pow2(127 - kSecondTop + ev[j] - 127);
+    double me[4], ve[4];
+    uint32_t tm = 0, tv = 0;
+#pragma unroll
+    for (int q = 0; q < 4; ++q) {
+      const uint32_t mq = (mc >> (8 * q)) & 255u, vq = (vc >> (8 * q)) & 255u;
+      const double x = (double)ge[q];
+      me[q] = fma((double)__uint_as_float((mq & 127u) << 20 | (mq & 128u) << 24), fm, x * c1);
+      ve[q] = fma((double)__uint_as_float(vq << 20), fv, x * x * c2);
+      tm = larger(tm, upper_half(me[q]) & 0x7fffffffu);
+      tv = larger(tv, upper_half(ve[q]) & 0x7fffffffu);
+      pe[q] = adamw_move(pe[q], (float)me[q], (float)ve[q], k);
+    }
+    const int km = block_exponent(wave_largest(tm)), kv = block_exponent(wave_largest(tv));
+    mc = vc = 0;
+#pragma unroll
+    for (int q = 0; q < 4; ++q) {
+      const uint32_t r = adamw_mix((uint32_t)(i + q) ^ key);
+      const uint32_t hm = upper_half(me[q]), hv = upper_half(ve[q]) & 0x7fffffffu;
+      const uint32_t cm = adamw_code<kFirstTop>(hm & 0x7fffffffu, km + 1023, r & 0xffffu) | (me[q] < 0.0 ? 128u : 0u);
+      uint32_t cv = adamw_code<kSecondTop>(hv, kv + 1023, r >> 16);
+      cv = ve[q] > 0.0 && cv == 0 ? 1u : cv;
+      mc |= cm << (8 * q);
+      vc |= cv << (8 * q);
+    }
+    if (lane == 0) {
+      e.m_exp[block] = (uint8_t)(km + 127);
+      e.v_exp[block] = (uint8_t)(kv + 127);
+    }
+    if (whole) {
+      *(float4*)(p + i) = make_float4(pe[0], pe[1], pe[2], pe[3]);
+      *(uint32_t*)(m + i) = mc;
+      *(uint32_t*)(v + i) = vc;
+      if (copy) {
+        const u32x2 c = {adamw_bf16(pe[0]) | adamw_bf16(pe[1]) << 16, adamw_bf16(pe[2]) | adamw_bf16(pe[3]) << 16};
+        *(u32x2*)(copy + i) = c;
+      }
+    } else {
+#pragma unroll
+      for (int q = 0; q < 4; ++q)
+        if (i + q < n) {
+          p[i + q] = pe[q];
+          m[i + q] = (uint8_t)(mc >> (8 * q));
+          v[i + q] = (uint8_t)(vc >> (8 * q));
+          if (copy) copy[i + q] = (uint16_t)adamw_bf16(pe[q]);
+        }
+    }
+  }
+}
+
+// A code's value in fp32: the exact product with 2^(127 - F') first, which takes it out of the denormals, then with 2^k.
+template <int TOP>
+__global__ void __launch_bounds__(256) k_adamw_values(const uint8_t* codes, const uint8_t* exps, int64_t n, float* out) {
+  const float lift = __uint_as_float((uint32_t)(254 - TOP) << 23);
+  for (int64_t i = ((int64_t)blockIdx.x * 256 + threadIdx.x) * 4; i < n; i += (int64_t)gridDim.x * 1024) {
+    const float scale = __uint_as_float((uint32_t)exps[i / kAdamwBlock] << 23);
+    float x[4];
+    uint32_t c = 0;
+    const bool whole = i + 4 <= n && !(((uintptr_t)codes & 3) | ((uintptr_t)out & 15));
+    if (whole) {
+      c = *(const uint32_t*)(codes + i);
+    } else {
+#pragma unroll
+      for (int q = 0; q < 4; ++q) c |= (i + q < n ? (uint32_t)codes[i + q] : 0u) << (8 * q);
+    }
+#pragma unroll
+    for (int q = 0; q < 4; ++q) {
+      const uint32_t b = (c >> (8 * q)) & 255u;
+      x[q] = __uint_as_float(TOP == kFirstTop ? (b & 127u) << 20 | (b & 128u) << 24 : b << 20) * lift * scale;
+    }
+    if (whole) {
+      *(float4*)(out + i) = make_float4(x[0], x[1], x[2], x[3]);
+    } else {
+#pragma unroll
+      for (int q = 0; q < 4; ++q)
+        if (i + q < n) out[i + q] = x[q];
+    }
+  }
+}
+
+void launch_adamw_32(const AdamwArgs& a, hipStream_t s) {
+  if (a.grad_bf16) hipLaunchKernelGGL(k_adamw_32<true>, dim3((unsigned)a.nchunks), dim3(256), 0, s, a);
+  else hipLaunchKernelGGL(k_adamw_32<false>, dim3((unsigned)a.nchunks), dim3(256), 0, s, a);
+}
+void launch_adamw_8(const AdamwArgs& a, hipStream_t s) {
+  if (a.grad_bf16) hipLaunchKernelGGL(k_adamw_8<true>, dim3((unsigned)a.nchunks), dim3(256), 0, s, a);
+  else hipLaunchKernelGGL(k_adamw_8<false>, dim3((unsigned)a.nchunks), dim3(256), 0, s, a);
+}
+void launch_adamw_values(int moment, const uint8_t* codes, const uint8_t* exps, int64_t n, float* out, hipStream_t s) {
+  const int64_t groups = (n + 1023) / 1024, most = 1 << 20;
+  const dim3 grid((unsigned)(groups < most ? groups : most));
+  if (moment == FASTCLIP_ADAMW_FIRST)
+    hipLaunchKernelGGL(k_adamw_values<kFirstTop>, grid, dim3(256), 0, s, codes, exps, n, out);
+  else
+    hipLaunchKernelGGL(k_adamw_values<kSecondTop>, grid, dim3(256), 0, s, codes, exps, n, out);
+}
+
+}  // namespace fc

@@ -1,0 +1,313 @@
+// Products of linear layers on the bf16 matrix cores (gfx950, wave64, MFMA 32x32x16): forward, gradient of the input, gradient
+// of the weight, each with what belongs to it in its epilogue.
+//
+//   out[m, n] = sum_k P[m, k] Q[n, k]
+//
+// An operand lies by rows (k contiguous) or by depth (k is the matrix's row).  Both come into LDS as they lie, by direct-to-LDS
+// loads, 64 of k a stage; by rows an MFMA operand is one 16-byte read, by depth two transposing reads.  Q gives the MFMA's rows
+// and P its columns, so that a lane holds four neighbouring columns of an output row; lanes 32 apart exchange halves, and every
+// load and store of the epilogue is eight neighbouring values.
+//
+// Edges: rows beyond M (columns beyond N) repeat the last one, and what they produce is not stored.  Depth beyond K has to add
+// nothing whatever the matrices hold, so the last stage takes its words from a block of zeros.
+#include "linear_common.hpp"
+
+namespace fc {
+
+constexpr int kDepth = 64;                       // of a stage
+__device__ __align__(16) uint32_t g_zero_words[4] = {0, 0, 0, 0};
+
+// 16 bytes per lane from an address of its own into LDS at lds_byte_addr + 16 * lane (wave-uniform address)
+__device__ __forceinline__ void dma16_from(const void* lane_address, uint32_t lds_byte_addr) {
+  asm volatile("s_mov_b32 m0, %1\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %0, off"
+               :
+               : "v"(lane_address), "s"(__builtin_amdgcn_readfirstlane(lds_byte_addr))
+               : "memory");
+}
+
+// LDS image of an operand by rows, 128 bytes a row: 16-byte chunk c of row r at position c ^ ((r >> 1) & 7), so that the 16
+// rows which a read touches per cycle cover the banks.
+__device__ __forceinline__ int row_swizzle(int row) { return (row >> 1) & 7; }
+// LDS image of an operand by depth, T columns = T / 8 pieces a row of k: pieces moved by multiples of four, so that the 4 rows x
+// 64 bytes which a transposing read touches per cycle cover the banks.
+template <int T>
+__device__ __forceinline__ int depth_swizzle(int k) { return T == 64 ? ((k >> 1) & 1) << 2 : (k & 3) << 2; }
+
+// One operand of a tile: T rows (columns) of the output from `first` on, WAVES wavefronts fetching.
+template <int T, bool BY_DEPTH, int WAVES>
+struct Operand {
+  static constexpr int kLoads = T / 8 / WAVES;   // wave loads of 1 KiB per wavefront and stage
+  static constexpr int kBytes = T * kDepth * 2;
+  const bf16_t* base;                            // of the tile, at depth 0 (wave-uniform)
+  int64_t ld;
+  int lane, wave;
+  uint32_t off[kLoads];                          // byte offset of this lane's words of a stage
+  __device__ __forceinline__ int pieces() const { return T / 8; }
+  // row of k (by depth) or chunk of k (by rows) inside a stage that this lane fetches with load i
+  __device__ __forceinline__ int depth_of(int i) const {
+    const int f = wave * kLoads + i;
+    if constexpr (BY_DEPTH) return f * (64 / (T / 8)) + lane / (T / 8);
+    return 8 * ((lane & 7) ^ row_swizzle(8 * f + (lane >> 3)));
+  }
+  __device__ __forceinline__ void open(const bf16_t* matrix, int64_t ld_, int64_t first, int64_t count, int lane_, int wave_) {
+    ld = ld_; lane = lane_; wave = wave_;
+    base = matrix + (BY_DEPTH ? first : first * ld);
+    const int left = (int)(count - first < T ? count - first : T);          // rows (columns) of the tile that exist
+#pragma unroll
+    for (int i = 0; i < kLoads; ++i) {
+      const int f = wave * kLoads + i, d = depth_of(i);
+      if constexpr (BY_DEPTH) {
+        int piece = (lane % (T / 8)) ^ depth_swizzle<T>(d);
+        piece = piece * 8 < left ? piece : left / 8 - 1;
+        off[i] = (uint32_t)d * (uint32_t)ld * 2u + (uint32_t)piece * 16u;
+      } else {
+        int row = 8 * f + (lane >> 3);
+        row = row < left ? row : left - 1;
+        off[i] = (uint32_t)row * (uint32_t)ld * 2u + (uint32_t)d * 2u;
+      }
+    }
+  }
+  // requests the 64 of k from k0 on into the panel at lds; what lies at or beyond `end` comes as zeros
+  __device__ __forceinline__ void request(int64_t k0, int64_t end, uint32_t lds) const {
+    const bf16_t* at = base + (BY_DEPTH ? k0 * ld : k0);
+    const uint32_t to = lds + (uint32_t)(wave * kLoads) * 1024u;
+    if (k0 + kDepth <= end) {
+#pragma unroll
+      for (int i = 0; i < kLoads; ++i) dma16(at, off[i], to + (uint32_t)i * 1024u);
+    } else {
+#pragma unroll
+      for (int i = 0; i < kLoads; ++i) {
+        const bool in = k0 + depth_of(i) < end;
+        dma16_from(in ? (const char*)at + off[i] : (const char*)g_zero_words, to + (uint32_t)i * 1024u);
+      }
+    }
+  }
+  // MFMA operand: rows (columns) 32 t .. of the panel, k = 16 s + 8 (lane >> 5) ..
+  __device__ __forceinline__ bf16x8 read(const char* panel, int t, int s) const {
+    const int lr = lane & 31, h = lane >> 5;
+    if constexpr (BY_DEPTH) {
+      const int n = 32 * t + ((lane >> 4) & 1) * 16 + 4 * (lane & 3), k = 16 * s + 8 * h + ((lane & 15) >> 2);
+      u32x2 half[2];
+#pragma unroll
+      for (int j = 0; j < 2; ++j) {
+        const char* p = panel + (k + 4 * j) * (T * 2) + (((n >> 3) ^ depth_swizzle<T>(k + 4 * j)) << 4) + ((n & 7) << 1);
+        half[j] = __builtin_bit_cast(u32x2, __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_v4s*)(uintptr_t)lds_addr(p)));
+      }
+      return join_halves(half[0], half[1]);
+    } else {
+      const int r = 32 * t + lr;
+      return *(const bf16x8*)(panel + r * 128 + (((2 * s + h) ^ row_swizzle(r)) << 4));
+    }
+  }
+};
+
+// Lanes l < 32 and l + 32 hold columns 8 g + 4 (l >> 5) .. + 3 of a row for g = 2 p, 2 p + 1: afterwards the first holds columns
+// 16 p .. + 7 and the second 16 p + 8 .. + 15.
+__device__ __forceinline__ void exchange_halves(float (&v)[8]) {
+#pragma unroll
+  for (int q = 0; q < 4; ++q) {
+    const auto r = __builtin_amdgcn_permlane32_swap(__float_as_uint(v[q]), __float_as_uint(v[4 + q]), false, false);
+    v[q] = __uint_as_float(r[0]);
+    v[4 + q] = __uint_as_float(r[1]);
+  }
+}
+
+// WN x WM wavefronts, each with NI x NJ blocks of 32 x 32: 32 NI WN columns by 32 NJ WM rows of the output, S stages in flight.
+template <bool PD, bool QD, int NI, int NJ, int WN, int WM, int S>
+__global__ void __launch_bounds__(64 * WN * WM) k_linear_bf16(LinearArgs a, uint32_t tiles_m, uint32_t tiles_n, int64_t slice) {
+  constexpr int TN = 32 * NI * WN, TM = 32 * NJ * WM, WAVES = WN * WM;
+  typedef Operand<TM, PD, WAVES> OpP;
+  typedef Operand<TN, QD, WAVES> OpQ;
+  constexpr int kStage = OpP::kBytes + OpQ::kBytes, kRequests = OpP::kLoads + OpQ::kLoads;
+  __shared__ __attribute__((aligned(1024))) char ring[S * kStage];
+  const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+  const int wn = wave % WN, wm = wave / WN, lr = lane & 31, hk = lane >> 5;
+  const TilePlace place = tile_place(blockIdx.x, gridDim.x, tiles_m, tiles_n);
+  const int64_t m0 = place.m * TM, n0 = place.n * TN, k0 = place.split * slice;
+  const int64_t end = k0 + slice < a.K ? k0 + slice : a.K;
+  const int stages = (int)((end - k0 + kDepth - 1) / kDepth);
+  OpP p;
+  OpQ q;
+  p.open((const bf16_t*)a.p, a.ldp, m0, a.M, lane, wave);
+  q.open((const bf16_t*)a.q, a.ldq, n0, a.N, lane, wave);
+  const uint32_t ring_at = lds_addr(ring);
+  auto request = [&](int stage) {
+    const uint32_t slot = ring_at + (uint32_t)(stage % S) * (uint32_t)kStage;
+    p.request(k0 + (int64_t)stage * kDepth, end, slot);
+    q.request(k0 + (int64_t)stage * kDepth, end, slot + (uint32_t)OpP::kBytes);
+  };
+  f32x16 acc[NI][NJ];
+#pragma unroll
+  for (int i = 0; i < NI; ++i)
+#pragma unroll
+    for (int j = 0; j < NJ; ++j)
+#pragma unroll
+      for (int v = 0; v < 16; ++v) acc[i][j][v] = 0.f;
+  const bool sums = PD && QD && a.dbias && place.n == 0 && wn == 0;      // this wavefront also sums P over the depth
+  float total[NJ];
+#pragma unroll
+  for (int j = 0; j < NJ; ++j) total[j] = 0.f;
+
+#pragma unroll
+  for (int s = 0; s < S - 1; ++s)
+    if (s < stages) request(s);
+  for (int g = 0; g < stages; ++g) {
+    // stage g has landed, and every wavefront is done with stage g - 1, whose place the next request takes
+    if (g + S - 2 < stages) wait_vmcnt<(S - 2) * kRequests>();
+    else FC_WAIT_VMCNT0();
+    FC_FENCE();
+    __builtin_amdgcn_s_barrier();
+    FC_FENCE();
+    if (g + S - 1 < stages) request(g + S - 1);
+    const char* panel_p = ring + (g % S) * kStage;
+    const char* panel_q = panel_p + OpP::kBytes;
+    float some[NJ];
+#pragma unroll
+    for (int j = 0; j < NJ; ++j) some[j] = 0.f;
+#pragma unroll
+    for (int s = 0; s < kDepth / 16; ++s) {
+      bf16x8 x[NJ], y[NI];
+#pragma unroll
+      for (int j = 0; j < NJ; ++j) x[j] = p.read(panel_p, wm * NJ + j, s);
+#pragma unroll
+      for (int i = 0; i < NI; ++i) y[i] = q.read(panel_q, wn * NI + i, s);
+#pragma unroll
+      for (int i = 0; i < NI; ++i)
+#pragma unroll
+        for (int j = 0; j < NJ; ++j) acc[i][j] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(y[i], x[j], acc[i][j], 0, 0, 0);
+      if constexpr (PD && QD) {
+        if (sums) {
+          const bf16x2 ones = __builtin_bit_cast(bf16x2, 0x3f803f80u);
+#pragma unroll
+          for (int j = 0; j < NJ; ++j) {
+            const u32x4 w = __builtin_bit_cast(u32x4, x[j]);
+#pragma unroll
+            for (int e = 0; e < 4; ++e) {
+              const uint32_t pair = w[e];        // a bit cast of a vector's element itself takes the first one
+              some[j] = __builtin_amdgcn_fdot2_f32_bf16(__builtin_bit_cast(bf16x2, pair), ones, some[j], false);
+            }
+          }
+        }
+      }
+    }
+    if constexpr (PD && QD) {
+#pragma unroll
+      for (int j = 0; j < NJ; ++j) total[j] += some[j];
+    }
+  }
+
+  const bool split = gridDim.x > tiles_m * tiles_n;
+  if (sums) {
+#pragma unroll
+    for (int j = 0; j < NJ; ++j) {
+      const float s = total[j] + __shfl_xor(total[j], 32);
+      const int64_t m = m0 + (wm * NJ + j) * 32 + lr;
+      float* to = split ? a.partial + (int64_t)(gridDim.x / (tiles_m * tiles_n)) * a.M * a.N + place.split * a.M : a.dbias;
+      if (hk == 0 && m < a.M) to[m] = s;
+    }
+  }
+#pragma unroll
+  for (int j = 0; j < NJ; ++j) {
+    const int64_t m = m0 + (wm * NJ + j) * 32 + lr;
+#pragma unroll
+    for (int i = 0; i < NI; ++i)
+#pragma unroll
+      for (int h = 0; h < 2; ++h) {
+        float v[8];
+#pragma unroll
+        for (int e = 0; e < 8; ++e) v[e] = acc[i][j][8 * h + e];
+        exchange_halves(v);
+        const int64_t n = n0 + (wn * NI + i) * 32 + 16 * h + 8 * hk;
+        if (m < a.M && n < a.N) {
+          if (split) store_f32<8>(a.partial + ((int64_t)place.split * a.M + m) * a.N + n, v);
+          else finish_values<true, 8>(a, v, m, n);
+        }
+      }
+  }
+}
+
+// ---- sums of splits -----------------------------------------------------------------------------------------------------
+template <bool BF16, int V>
+__global__ void __launch_bounds__(256) k_linear_join(LinearArgs a, int splits) {
+  const int64_t per_row = a.N / V, total = a.M * per_row;
+  const int64_t t = (int64_t)blockIdx.x * 256 + threadIdx.x;
+  if (t < total) {
+    const int64_t m = t / per_row, n = (t - m * per_row) * V;
+    float z[V];
+#pragma unroll
+    for (int i = 0; i < V; ++i) z[i] = 0.f;
+#pragma unroll 4
+    for (int s = 0; s < splits; ++s) {
+      float x[V];
+      load_f32<V>(x, a.partial + ((int64_t)s * a.M + m) * a.N + n);
+#pragma unroll
+      for (int i = 0; i < V; ++i) z[i] += x[i];
+    }
+    finish_values<BF16, V>(a, z, m, n);
+  } else if (a.dbias && t - total < a.M) {
+    const int64_t m = t - total;
+    const float* part = a.partial + (int64_t)splits * a.M * a.N + m;
+    float z = 0.f;
+#pragma unroll 4
+    for (int s = 0; s < splits; ++s) z += part[(int64_t)s * a.M];
+    a.dbias[m] = z;
+  }
+}
+
+void launch_linear_join(const LinearArgs& a, const LinearPlan& plan, hipStream_t s) {
+  const int v = a.bf16 ? 8 : 1;
+  const int64_t threads = a.M * (a.N / v) + (a.dbias ? a.M : 0);
+  const dim3 grid((unsigned)((threads + 255) / 256));
+  if (a.bf16) hipLaunchKernelGGL((k_linear_join<true, 8>), grid, dim3(256), 0, s, a, plan.splits);
+  else hipLaunchKernelGGL((k_linear_join<false, 1>), grid, dim3(256), 0, s, a, plan.splits);
+}
+
+// The gradient of the weight of no rows.
+__global__ void __launch_bounds__(256) k_linear_empty(LinearArgs a) {
+  for (int64_t t = (int64_t)blockIdx.x * 256 + threadIdx.x; t < a.M * a.N; t += (int64_t)gridDim.x * 256) {
+    const int64_t m = t / a.N, n = t - m * a.N;
+    if (a.out_bf16) ((bf16_t*)a.out)[m * a.ld_out + n] = 0;
+    else ((float*)a.out)[m * a.ld_out + n] = 0.f;
+    if (a.dbias && n == 0) a.dbias[m] = 0.f;
+  }
+}
+void launch_linear_empty(const LinearArgs& a, hipStream_t s) {
+  hipLaunchKernelGGL(k_linear_empty, dim3(1024), dim3(256), 0, s, a);
+}
+
+// ---- plan -----------------------------------------------------------------------------------------------------------------
+LinearPlan plan_linear(int64_t M, int64_t N, int64_t K, bool bf16, bool, bool, bool dbias) {
+  LinearPlan best = {64, 1, K, 0};
+  auto tiles = [&](int64_t t) { return ((M + t - 1) / t) * ((N + t - 1) / t); };
+  if (bf16) best.tile = tiles(256) >= 192 ? 256 : (tiles(128) >= 192 ? 128 : 64);
+  const int64_t stages = (K + kDepth - 1) / kDepth, n = tiles(best.tile);
+  int64_t splits = best.tile < 256 && n < 256 ? 512 / n : 1;
+  if (splits > stages / 4) splits = stages / 4;
+  while (splits > 1 && splits * M * N > ((int64_t)16 << 20)) --splits;
+  if (splits < 1) splits = 1;
+  const int64_t slice = (stages + splits - 1) / splits;
+  best.splits = (int)((stages + slice - 1) / slice);
+  best.slice = slice * kDepth;
+  if (best.splits > 1) best.bytes = round_up(sizeof(float) * (size_t)best.splits * (size_t)(M * N + (dbias ? M : 0)), 256);
+  return best;
+}
+
+template <bool PD, bool QD>
+static void launch_form(const LinearArgs& a, const LinearPlan& plan, hipStream_t s) {
+  const uint32_t tm = (uint32_t)((a.M + plan.tile - 1) / plan.tile), tn = (uint32_t)((a.N + plan.tile - 1) / plan.tile);
+  const dim3 grid(tm * tn * (uint32_t)plan.splits);
+  if (plan.tile == 256)
+    hipLaunchKernelGGL((k_linear_bf16<PD, QD, 2, 4, 4, 2, 2>), grid, dim3(512), 0, s, a, tm, tn, plan.slice);
+  else if (plan.tile == 128)
+    hipLaunchKernelGGL((k_linear_bf16<PD, QD, 2, 2, 2, 2, 2>), grid, dim3(256), 0, s, a, tm, tn, plan.slice);
+  else
+    hipLaunchKernelGGL((k_linear_bf16<PD, QD, 1, 1, 2, 2, 3>), grid, dim3(256), 0, s, a, tm, tn, plan.slice);
+}
+
+void launch_linear_bf16(const LinearArgs& a, const LinearPlan& plan, hipStream_t s) {
+  if (a.p_by_depth) launch_form<true, true>(a, plan, s);
+  else if (a.q_by_depth) launch_form<false, true>(a, plan, s);
+  else launch_form<false, false>(a, plan, s);
+}
+
+}  // namespace fc

@@ -1,0 +1,435 @@
+// Layer norm over rows, forward and backward (gfx950, wave64).
+//
+//   mean = sum x / d,  rstd = 1 / sqrt(sum (x - mean)^2 / d + eps),  y = (x - mean) rstd w + b
+//   xh = (x - mean) rstd,  q = dy w:  dx = rstd (q - sum q / d - xh sum (q xh) / d),  dw = sum_r dy xh,  db = sum_r dy
+//
+// Both passes are bound by memory: a row is read once, stays in registers (16 values a lane at most) while its sums are formed -
+// the squares around the mean that is already known, so that a mean far from zero costs no digits - and is written once.  A
+// wavefront takes a row of up to 1024, a workgroup of four one of up to 4096; longer rows are read once per sum.  Workgroups
+// stay and go through the rows, so that weight and bias are read once, the next row is requested before the present one is
+// summed, and the backward pass keeps its sums over the rows in registers: a workgroup leaves one partial sum per column, which
+// a second kernel adds up in a fixed order.
+#include "operators.hpp"
+
+namespace fc {
+
+typedef __attribute__((__vector_size__(4 * sizeof(uint32_t)))) uint32_t u32x4;
+
+__device__ __forceinline__ float norm_from_bits(uint16_t x) { return __uint_as_float((uint32_t)x << 16); }
+__device__ __forceinline__ uint16_t norm_to_bits(float x) { return __builtin_bit_cast(uint16_t, (__bf16)x); }
+
+// VEC consecutive elements of a row as they lie in memory
+template <typename T, int VEC>
+struct Packed;
+template <>
+struct Packed<float, 8> {
+  u32x4 lo, hi;
+  __device__ void load(const float* p) { lo = *(const u32x4*)p; hi = *(const u32x4*)(p + 4); }
+  __device__ void clear() { lo = hi = u32x4{0, 0, 0, 0}; }
+  __device__ float get(int i) const { return __uint_as_float(i < 4 ? lo[i & 3] : hi[i & 3]); }
+  static __device__ void store(float* p, const float (&v)[8]) {
+    *(float4*)p = make_float4(v[0], v[1], v[2], v[3]);
+    *(float4*)(p + 4) = make_float4(v[4], v[5], v[6], v[7]);
+  }
+};
+template <>
+struct Packed<bf16_t, 8> {
+  u32x4 w;
+  __device__ void load(const bf16_t* p) { w = *(const u32x4*)p; }
+  __device__ void clear() { w = u32x4{0, 0, 0, 0}; }
+  __device__ float get(int i) const { return __uint_as_float(i & 1 ? w[i >> 1] & 0xffff0000u : w[i >> 1] << 16); }
+  static __device__ void store(bf16_t* p, const float (&v)[8]) {
+    u32x4 r;
+#pragma unroll
+    for (int i = 0; i < 4; ++i) r[i] = (uint32_t)norm_to_bits(v[2 * i]) | ((uint32_t)norm_to_bits(v[2 * i + 1]) << 16);
+    *(u32x4*)p = r;
+  }
+};
+template <>
+struct Packed<float, 1> {
+  float w;
+  __device__ void load(const float* p) { w = *p; }
+  __device__ void clear() { w = 0.f; }
+  __device__ float get(int) const { return w; }
+  static __device__ void store(float* p, const float (&v)[1]) { *p = v[0]; }
+};
+template <>
+struct Packed<bf16_t, 1> {
+  uint16_t w;
+  __device__ void load(const bf16_t* p) { w = *p; }
+  __device__ void clear() { w = 0; }
+  __device__ float get(int) const { return norm_from_bits(w); }
+  static __device__ void store(bf16_t* p, const float (&v)[1]) { *p = norm_to_bits(v[0]); }
+};
+
+__device__ __forceinline__ float wave_sum(float x) {
+#pragma unroll
+  for (int m = 32; m > 0; m >>= 1) x += __shfl_xor(x, m);
+  return x;
+}
+
+// Sum over the W wavefronts of a row.  red: one float per wavefront, another array for every sum in flight: a wavefront that
+// writes one again has passed the barrier of the sum in between, behind which every wavefront had read it.
+template <int W>
+__device__ __forceinline__ float row_sum(float x, float* red) {
+  x = wave_sum(x);
+  if constexpr (W > 1) {
+    if ((threadIdx.x & 63) == 0) red[threadIdx.x >> 6] = x;
+    __syncthreads();
+    x = 0.f;
+#pragma unroll
+    for (int w = 0; w < W; ++w) x += red[w];
+  }
+  return x;
+}
+
+template <int VEC, int NC, int T>
+__device__ __forceinline__ void load_columns(float (&v)[NC][VEC], const float* p, float other, int lane, int64_t d) {
+#pragma unroll
+  for (int j = 0; j < NC; ++j) {
+    const int64_t c = (int64_t)(lane + T * j) * VEC;
+    Packed<float, VEC> w;
+    w.clear();
+    if (p && c < d) w.load(p + c);
+#pragma unroll
+    for (int i = 0; i < VEC; ++i) v[j][i] = p ? w.get(i) : other;
+  }
+}
+
+template <typename X, int VEC, int NC, int T>
+__device__ __forceinline__ void load_row(Packed<X, VEC> (&v)[NC], const X* row, int lane, int64_t d) {
+#pragma unroll
+  for (int j = 0; j < NC; ++j) {
+    const int64_t c = (int64_t)(lane + T * j) * VEC;
+    v[j].clear();
+    if (c < d) v[j].load(row + c);
+  }
+}
+
+template <typename X, typename Y, int VEC, int NC, int W>
+__global__ void __launch_bounds__(256) k_layer_norm_forward(NormArgs a) {
+  constexpr int T = 64 * W, R = 4 / W;
+  __shared__ float red[2][4];
+  const int lane = threadIdx.x % T;
+  const int64_t step = (int64_t)gridDim.x * R;
+  int64_t row = (int64_t)blockIdx.x * R + threadIdx.x / T;
+  if (row >= a.rows) return;                      // whole wavefronts, with W > 1 whole workgroups
+  const X* x = (const X*)a.x;
+  Packed<X, VEC> cur[NC], next[NC];
+  load_row<X, VEC, NC, T>(cur, x + row * a.ld_x, lane, a.d);
+  float w[NC][VEC], b[NC][VEC];
+  load_columns<VEC, NC, T>(w, a.weight, 1.f, lane, a.d);
+  load_columns<VEC, NC, T>(b, a.bias, 0.f, lane, a.d);
+  const float d = (float)a.d;      // divided by, not multiplied with 1 / d: a constant row's mean is that constant
+  for (; row < a.rows; row += step) {
+    const bool more = row + step < a.rows;
+    if (more) load_row<X, VEC, NC, T>(next, x + (row + step) * a.ld_x, lane, a.d);
+    float s = 0.f;
+#pragma unroll
+    for (int j = 0; j < NC; ++j)
+#pragma unroll
+      for (int i = 0; i < VEC; ++i) s += cur[j].get(i);
+    const float mean = row_sum<W>(s, red[0]) / d;
+    float q = 0.f;
+#pragma unroll
+    for (int j = 0; j < NC; ++j) {
+      const bool in = (int64_t)(lane + T * j) * VEC < a.d;
+#pragma unroll
+      for (int i = 0; i < VEC; ++i) {
+        const float off = in ? cur[j].get(i) - mean : 0.f;
+        q = fmaf(off, off, q);
+      }
+    }
+    const float rstd = 1.f / sqrtf(row_sum<W>(q, red[1]) / d + a.eps);
+    Y* y = (Y*)a.out + row * a.ld_y;
+#pragma unroll
+    for (int j = 0; j < NC; ++j) {
+      const int64_t c = (int64_t)(lane + T * j) * VEC;
+      float v[VEC];
+#pragma unroll
+      for (int i = 0; i < VEC; ++i) v[i] = fmaf((cur[j].get(i) - mean) * rstd, w[j][i], b[j][i]);
+      if (c < a.d) Packed<Y, VEC>::store(y + c, v);
+    }
+    if (lane == 0) {
+      if (a.mean) a.mean[row] = mean;
+      if (a.rstd) a.rstd[row] = rstd;
+    }
+    if (more) {
+#pragma unroll
+      for (int j = 0; j < NC; ++j) cur[j] = next[j];
+    }
+  }
+}
+
+template <typename X, typename Y, int VEC, int NC, int W>
+__global__ void __launch_bounds__(256) k_layer_norm_backward(NormArgs a) {
+  constexpr int T = 64 * W, R = 4 / W;
+  __shared__ float red[2][2][4];
+  __shared__ float columns[W == 1 ? 4 * 64 * NC * VEC : 1];
+  const int lane = threadIdx.x % T;
+  const int64_t step = (int64_t)gridDim.x * R, first = (int64_t)blockIdx.x * R + threadIdx.x / T;
+  const X* x = (const X*)a.x;
+  const Y* dy = (const Y*)a.dy;
+  float w[NC][VEC], dw[NC][VEC], db[NC][VEC];
+  load_columns<VEC, NC, T>(w, a.weight, 1.f, lane, a.d);
+#pragma unroll
+  for (int j = 0; j < NC; ++j)
+#pragma unroll
+    for (int i = 0; i < VEC; ++i) dw[j][i] = db[j][i] = 0.f;
+  const float d = (float)a.d;
+  Packed<X, VEC> cx[NC], nx[NC];
+  Packed<Y, VEC> cy[NC], ny[NC];
+  float cm = 0.f, cr = 0.f, nm = 0.f, nr = 0.f;
+  if (first < a.rows) {
+    load_row<X, VEC, NC, T>(cx, x + first * a.ld_x, lane, a.d);
+    load_row<Y, VEC, NC, T>(cy, dy + first * a.ld_y, lane, a.d);
+    cm = a.mean[first];
+    cr = a.rstd[first];
+  }
+  int odd = 0;
+  for (int64_t row = first; row < a.rows; row += step, odd ^= 1) {
+    const bool more = row + step < a.rows;
+    if (more) {
+      load_row<X, VEC, NC, T>(nx, x + (row + step) * a.ld_x, lane, a.d);
+      load_row<Y, VEC, NC, T>(ny, dy + (row + step) * a.ld_y, lane, a.d);
+      nm = a.mean[row + step];
+      nr = a.rstd[row + step];
+    }
+    float s1 = 0.f, s2 = 0.f;
+    float xh[NC][VEC];
+#pragma unroll
+    for (int j = 0; j < NC; ++j) {
+      const bool in = (int64_t)(lane + T * j) * VEC < a.d;
+#pragma unroll
+      for (int i = 0; i < VEC; ++i) {
+        const float g = cy[j].get(i), q = g * w[j][i];
+        xh[j][i] = in ? (cx[j].get(i) - cm) * cr : 0.f;
+        s1 += q;
+        s2 = fmaf(q, xh[j][i], s2);
+        dw[j][i] = fmaf(g, xh[j][i], dw[j][i]);
+        db[j][i] += g;
+      }
+    }
+    if constexpr (W == 1) {
+      s1 = wave_sum(s1);
+      s2 = wave_sum(s2);
+    } else {
+      s1 = wave_sum(s1);
+      s2 = wave_sum(s2);
+      if ((threadIdx.x & 63) == 0) {
+        red[odd][0][threadIdx.x >> 6] = s1;
+        red[odd][1][threadIdx.x >> 6] = s2;
+      }
+      __syncthreads();
+      s1 = s2 = 0.f;
+#pragma unroll
+      for (int k = 0; k < W; ++k) {
+        s1 += red[odd][0][k];
+        s2 += red[odd][1][k];
+      }
+    }
+    s1 /= d;
+    s2 /= d;
+    X* dx = (X*)a.out + row * a.ld_x;
+#pragma unroll
+    for (int j = 0; j < NC; ++j) {
+      const int64_t c = (int64_t)(lane + T * j) * VEC;
+      float v[VEC];
+#pragma unroll
+      for (int i = 0; i < VEC; ++i) v[i] = cr * (cy[j].get(i) * w[j][i] - s1 - xh[j][i] * s2);
+      if (c < a.d) Packed<X, VEC>::store(dx + c, v);
+    }
+    if (more) {
+#pragma unroll
+      for (int j = 0; j < NC; ++j) { cx[j] = nx[j]; cy[j] = ny[j]; }
+      cm = nm;
+      cr = nr;
+    }
+  }
+  // this workgroup's sums over its rows
+  float* part = a.partial + (int64_t)blockIdx.x * 2 * a.d;
+#pragma unroll
+  for (int which = 0; which < 2; ++which) {
+    if constexpr (W == 1) {
+      __syncthreads();
+#pragma unroll
+      for (int j = 0; j < NC; ++j)
+#pragma unroll
+        for (int i = 0; i < VEC; ++i)
+          columns[((threadIdx.x >> 6) * NC * VEC + j * VEC + i) * 64 + lane] = which ? db[j][i] : dw[j][i];
+      __syncthreads();
+      for (int e = threadIdx.x; e < 64 * NC * VEC; e += 256) {       // e = (j VEC + i) 64 + lane
+        const int l = e & 63, i = (e >> 6) % VEC, j = (e >> 6) / VEC;
+        const int64_t c = (int64_t)(l + 64 * j) * VEC + i;
+        float s = 0.f;
+#pragma unroll
+        for (int k = 0; k < 4; ++k) s += columns[k * 64 * NC * VEC + e];
+        if (c < a.d) part[which * a.d + c] = s;
+      }
+    } else {
+#pragma unroll
+      for (int j = 0; j < NC; ++j)
+#pragma unroll
+        for (int i = 0; i < VEC; ++i) {
+          const int64_t c = (int64_t)(lane + T * j) * VEC + i;
+          if (c < a.d) part[which * a.d + c] = which ? db[j][i] : dw[j][i];
+        }
+    }
+  }
+}
+
+// Rows longer than registers hold: read once per sum, a workgroup a row.
+template <typename X, typename Y>
+__global__ void __launch_bounds__(256) k_layer_norm_forward_long(NormArgs a) {
+  __shared__ float red[2][4];
+  const float d = (float)a.d;
+  for (int64_t row = blockIdx.x; row < a.rows; row += gridDim.x) {
+    const X* x = (const X*)a.x + row * a.ld_x;
+    Y* y = (Y*)a.out + row * a.ld_y;
+    float s = 0.f, q = 0.f;
+    for (int64_t c = threadIdx.x; c < a.d; c += 256) {
+      Packed<X, 1> v;
+      v.load(x + c);
+      s += v.get(0);
+    }
+    const float mean = row_sum<4>(s, red[0]) / d;
+    for (int64_t c = threadIdx.x; c < a.d; c += 256) {
+      Packed<X, 1> v;
+      v.load(x + c);
+      const float off = v.get(0) - mean;
+      q = fmaf(off, off, q);
+    }
+    const float rstd = 1.f / sqrtf(row_sum<4>(q, red[1]) / d + a.eps);
+    for (int64_t c = threadIdx.x; c < a.d; c += 256) {
+      Packed<X, 1> v;
+      v.load(x + c);
+      const float r[1] = {fmaf((v.get(0) - mean) * rstd, a.weight ? a.weight[c] : 1.f, a.bias ? a.bias[c] : 0.f)};
+      Packed<Y, 1>::store(y + c, r);
+    }
+    if (threadIdx.x == 0) {
+      if (a.mean) a.mean[row] = mean;
+      if (a.rstd) a.rstd[row] = rstd;
+    }
+  }
+}
+
+// ... its partial sums over the rows gather in the workspace, where they are this workgroup's own.
+template <typename X, typename Y>
+__global__ void __launch_bounds__(256) k_layer_norm_backward_long(NormArgs a) {
+  __shared__ float red[2][4];
+  const float d = (float)a.d;
+  float* part = a.partial + (int64_t)blockIdx.x * 2 * a.d;
+  for (int64_t row = blockIdx.x; row < a.rows; row += gridDim.x) {
+    const X* x = (const X*)a.x + row * a.ld_x;
+    const Y* dy = (const Y*)a.dy + row * a.ld_y;
+    X* dx = (X*)a.out + row * a.ld_x;
+    const float mean = a.mean[row], rstd = a.rstd[row];
+    float s1 = 0.f, s2 = 0.f;
+    for (int64_t c = threadIdx.x; c < a.d; c += 256) {
+      Packed<X, 1> v;
+      Packed<Y, 1> g;
+      v.load(x + c);
+      g.load(dy + c);
+      const float xh = (v.get(0) - mean) * rstd, q = g.get(0) * (a.weight ? a.weight[c] : 1.f);
+      s1 += q;
+      s2 = fmaf(q, xh, s2);
+      const bool begun = row != blockIdx.x;
+      part[c] = fmaf(g.get(0), xh, begun ? part[c] : 0.f);
+      part[a.d + c] = g.get(0) + (begun ? part[a.d + c] : 0.f);
+    }
+    s1 = row_sum<4>(s1, red[0]) / d;
+    s2 = row_sum<4>(s2, red[1]) / d;
+    for (int64_t c = threadIdx.x; c < a.d; c += 256) {
+      Packed<X, 1> v;
+      Packed<Y, 1> g;
+      v.load(x + c);
+      g.load(dy + c);
+      const float xh = (v.get(0) - mean) * rstd, q = g.get(0) * (a.weight ? a.weight[c] : 1.f);
+      const float r[1] = {rstd * (q - s1 - xh * s2)};
+      Packed<X, 1>::store(dx + c, r);
+    }
+  }
+}
+
+// dweight and dbias: the workgroups' partial sums, 32 columns a workgroup, 32 threads a column.
+__global__ void __launch_bounds__(1024) k_layer_norm_columns(const float* partial, int groups, int64_t d, float* dweight,
+                                                             float* dbias) {
+  __shared__ float sums[32][33];
+  const int col = threadIdx.x & 31, part = threadIdx.x >> 5;
+  const int64_t c = (int64_t)blockIdx.x * 32 + col;
+  float s = 0.f;
+  if (c < 2 * d) {
+#pragma unroll 8
+    for (int g = part; g < groups; g += 32) s += partial[(int64_t)g * 2 * d + c];
+  }
+  sums[part][col] = s;
+  __syncthreads();
+  if (part == 0 && c < 2 * d) {
+    s = 0.f;
+#pragma unroll
+    for (int k = 0; k < 32; ++k) s += sums[k][col];
+    float* out = c < d ? dweight : dbias;
+    if (out) out[c < d ? c : c - d] = s;
+  }
+}
+
+constexpr int64_t kNormWave = 1024, kNormGroup = 4096;     // longest row of a wavefront and of a workgroup
+
+int layer_norm_groups(int64_t rows, int64_t d) {
+  const int64_t per = d <= kNormWave ? 4 : 1, most = d <= kNormWave ? 1024 : (d <= kNormGroup ? 512 : 256);
+  const int64_t groups = (rows + per - 1) / per;
+  return (int)(groups < most ? groups : most);
+}
+
+static bool rows_are_wide(const NormArgs& a) {
+  const uintptr_t ends = (uintptr_t)a.x | (uintptr_t)a.dy | (uintptr_t)a.weight | (uintptr_t)a.bias | (uintptr_t)a.out;
+  return a.d % 8 == 0 && !(ends & 15) && a.ld_x % (a.x_bf16 ? 8 : 4) == 0 && a.ld_y % (a.y_bf16 ? 8 : 4) == 0;
+}
+
+template <bool BACKWARD, typename X, typename Y>
+static void launch_rows(const NormArgs& a, int groups, hipStream_t s) {
+#define FC_ROWS(VEC, NC, W)                                                                                             \
+  do {                                                                                                                  \
+    if constexpr (BACKWARD) hipLaunchKernelGGL((k_layer_norm_backward<X, Y, VEC, NC, W>), dim3(groups), dim3(256), 0, s, a); \
+    else hipLaunchKernelGGL((k_layer_norm_forward<X, Y, VEC, NC, W>), dim3(groups), dim3(256), 0, s, a);                \
+  } while (0)
+  const bool wide = rows_are_wide(a);
+  if (a.d <= kNormWave) {
+    if (wide && a.d <= 512) FC_ROWS(8, 1, 1);
+    else if (wide) FC_ROWS(8, 2, 1);
+    else if (a.d <= 256) FC_ROWS(1, 4, 1);
+    else FC_ROWS(1, 16, 1);
+  } else if (a.d <= kNormGroup) {
+    if (wide && a.d <= 2048) FC_ROWS(8, 1, 4);
+    else if (wide) FC_ROWS(8, 2, 4);
+    else FC_ROWS(1, 16, 4);
+  } else {
+    if constexpr (BACKWARD) hipLaunchKernelGGL((k_layer_norm_backward_long<X, Y>), dim3(groups), dim3(256), 0, s, a);
+    else hipLaunchKernelGGL((k_layer_norm_forward_long<X, Y>), dim3(groups), dim3(256), 0, s, a);
+  }
+#undef FC_ROWS
+}
+
+template <bool BACKWARD>
+static void launch_types(const NormArgs& a, int groups, hipStream_t s) {
+  if (a.x_bf16 && a.y_bf16) launch_rows<BACKWARD, bf16_t, bf16_t>(a, groups, s);
+  else if (a.x_bf16) launch_rows<BACKWARD, bf16_t, float>(a, groups, s);
+  else if (a.y_bf16) launch_rows<BACKWARD, float, bf16_t>(a, groups, s);
+  else launch_rows<BACKWARD, float, float>(a, groups, s);
+}
+
+void launch_layer_norm_forward(const NormArgs& a, hipStream_t s) {
+  const int64_t per = a.d <= kNormWave ? 4 : 1, most = 2048;
+  const int64_t groups = (a.rows + per - 1) / per;
+  launch_types<false>(a, (int)(groups < most ? groups : most), s);
+}
+
+void launch_layer_norm_backward(const NormArgs& a, float* dweight, float* dbias, hipStream_t s) {
+  const int groups = layer_norm_groups(a.rows, a.d);
+  if (groups > 0) launch_types<true>(a, groups, s);
+  if (dweight || dbias)
+    hipLaunchKernelGGL(k_layer_norm_columns, dim3((unsigned)((2 * a.d + 31) / 32)), dim3(1024), 0, s, a.partial, groups, a.d,
+                       dweight, dbias);
+}
+
+}  // namespace fc

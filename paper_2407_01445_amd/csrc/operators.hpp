@@ -1,0 +1,89 @@
+// Internal declarations of the operators in front of the loss: layer norm, linear layers, AdamW (not part of the ABI).
+#pragma once
+#include "fc_internal.hpp"
+
+namespace fc {
+
+// ---- layer norm (kernels_norm.hip) ----------------------------------------------------------------------------------
+struct NormArgs {
+  const void* x;
+  const void* dy;
+  const float* weight;     // nullptr: ones
+  const float* bias;       // nullptr: zeros
+  void* out;               // y or dx
+  float* mean;             // forward: out or nullptr; backward: in
+  float* rstd;
+  float* partial;          // backward: [groups][2][d], sums of dy xh and of dy over a workgroup's rows
+  int64_t rows, d, ld_x, ld_y;
+  float eps;
+  bool x_bf16, y_bf16;
+};
+int layer_norm_groups(int64_t rows, int64_t d);     // workgroups of the backward pass = partial sums per column
+void launch_layer_norm_forward(const NormArgs& a, hipStream_t s);
+void launch_layer_norm_backward(const NormArgs& a, float* dweight, float* dbias, hipStream_t s);
+
+// ---- linear layers (kernels_linear.hip, kernels_linear_f32.hip) --------------------------------------------------------
+// One product out[m, n] = sum_k P[m, k] Q[n, k].  An operand lies either "by rows" (its k contiguous: x, w, dy as the left
+// side) or "by depth" (k the row of the matrix, m or n contiguous: dy and x of the weight's gradient, w of the input's).
+struct LinearArgs {
+  const void* p;           // operand of the output's rows
+  const void* q;           // operand of the output's columns
+  int64_t ldp, ldq;
+  bool p_by_depth, q_by_depth;
+  int64_t M, N, K;
+  void* out;
+  int64_t ld_out;
+  bool bf16, out_bf16;     // storage of the operands (and of pre), of out and residual
+  const float* bias;       // [N] or nullptr
+  const void* residual;    // [M, ld_res] or nullptr
+  int64_t ld_res;
+  void* pre_out;           // forward: [M, ld_pre] or nullptr
+  const void* pre_in;      // gradient of the input: [M, ld_pre] or nullptr
+  int64_t ld_pre;
+  int act;                 // fastclip_activation: of z, or of which the derivative is taken with pre_in
+  float* dbias;            // gradient of the weight: [M], sums of P over k, or nullptr
+  float* partial;          // workspace: [splits][M][N] and behind them [splits][M] for dbias
+};
+struct LinearPlan {
+  int tile;                // rows and columns of a workgroup's output tile
+  int splits;              // workgroups over the depth of a tile
+  int64_t slice;           // depth of a split
+  size_t bytes;            // workspace
+};
+LinearPlan plan_linear(int64_t M, int64_t N, int64_t K, bool bf16, bool p_by_depth, bool q_by_depth, bool dbias);
+void launch_linear_bf16(const LinearArgs& a, const LinearPlan& plan, hipStream_t s);
+void launch_linear_f32(const LinearArgs& a, const LinearPlan& plan, hipStream_t s);
+void launch_linear_join(const LinearArgs& a, const LinearPlan& plan, hipStream_t s);   // sums of the splits' partial results
+void launch_linear_empty(const LinearArgs& a, hipStream_t s);                          // no depth: zeros
+
+// ---- AdamW (kernels_adamw.hip) ------------------------------------------------------------------------------------------
+constexpr int kAdamwChunk = 4096;       // elements of a workgroup, whole blocks of 8-bit states
+constexpr int kAdamwBlock = 256;        // elements that share an exponent
+struct AdamwEntry {                     // a tensor in the device table
+  float* param;
+  const void* grad;
+  void* m;
+  void* v;
+  uint16_t* copy;
+  uint8_t* m_exp;
+  uint8_t* v_exp;
+  int64_t n;
+  float weight_decay;
+  int32_t wide;                         // every pointer 16-byte aligned
+};
+struct AdamwChunk { int32_t tensor, chunk; };
+struct AdamwArgs {
+  const AdamwEntry* entries;
+  const AdamwChunk* chunks;
+  int64_t nchunks;
+  bool grad_bf16;
+  float beta1, beta2, eps;
+  float lr, step_size;                  // lr / (1 - beta1^t)
+  float corr2;                          // 1 / (1 - beta2^t)
+  uint32_t seed;
+};
+void launch_adamw_32(const AdamwArgs& a, hipStream_t s);
+void launch_adamw_8(const AdamwArgs& a, hipStream_t s);
+void launch_adamw_values(int moment, const uint8_t* codes, const uint8_t* exps, int64_t n, float* out, hipStream_t s);
+
+}  // namespace fc

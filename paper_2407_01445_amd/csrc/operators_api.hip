@@ -1,0 +1,305 @@
+// C entry points of the operators in front of the loss (layer norm, linear layers, AdamW): argument checks, workspaces,
+// launch sequences.  The arithmetic is in the kernel translation units.
+#include <math.h>
+#include <string.h>
+
+#include "operators.hpp"
+
+namespace fc {
+
+static bool not_finite(float x) { return !(x == x) || isinf(x); }
+static bool known_type(int32_t t) { return t == FASTCLIP_F32 || t == FASTCLIP_BF16; }
+static bool aligned(const void* p, uintptr_t to) { return ((uintptr_t)p & (to - 1)) == 0; }
+static uintptr_t size_of(int32_t t) { return t == FASTCLIP_BF16 ? 2 : 4; }
+
+static fastclip_status check(const fastclip_layer_norm_config* c) {
+  if (!c) return FASTCLIP_ERR_NULL;
+  if (c->struct_size != sizeof(*c) || c->rows < 0 || c->d < 1 || c->ld_x < c->d || c->ld_y < c->d) return FASTCLIP_ERR_SHAPE;
+  if (!known_type(c->x_dtype) || !known_type(c->y_dtype) || not_finite(c->eps) || c->eps < 0.0f) return FASTCLIP_ERR_VALUE;
+  const int64_t lim = ((int64_t)1 << 31) - 1;
+  if (c->rows > lim || c->ld_x > lim || c->ld_y > lim) return FASTCLIP_ERR_UNSUPPORTED;
+  return FASTCLIP_OK;
+}
+
+static NormArgs norm_args(const fastclip_layer_norm_config& c) {
+  NormArgs a;
+  memset(&a, 0, sizeof(a));
+  a.rows = c.rows; a.d = c.d; a.ld_x = c.ld_x; a.ld_y = c.ld_y; a.eps = c.eps;
+  a.x_bf16 = c.x_dtype == FASTCLIP_BF16; a.y_bf16 = c.y_dtype == FASTCLIP_BF16;
+  return a;
+}
+
+static fastclip_status check(const fastclip_linear_config* c, int32_t pass) {
+  if (!c) return FASTCLIP_ERR_NULL;
+  if (c->struct_size != sizeof(*c) || c->rows < 0 || c->d_in < 1 || c->d_out < 1 || c->ld_x < c->d_in || c->ld_w < c->d_in ||
+      c->ld_y < c->d_out)
+    return FASTCLIP_ERR_SHAPE;
+  if (pass < FASTCLIP_LINEAR_FORWARD || pass > FASTCLIP_LINEAR_BACKWARD_WEIGHT || !known_type(c->dtype) ||
+      !known_type(c->out_dtype) || c->activation < FASTCLIP_ACT_NONE || c->activation > FASTCLIP_ACT_QUICK_GELU)
+    return FASTCLIP_ERR_VALUE;
+  const int64_t lim = (int64_t)1 << 22;
+  if (c->rows > ((int64_t)1 << 30) || c->ld_x > lim || c->ld_w > lim || c->ld_y > lim) return FASTCLIP_ERR_UNSUPPORTED;
+  if (c->dtype == FASTCLIP_BF16 && (c->d_in % 8 || c->d_out % 8 || c->ld_x % 8 || c->ld_w % 8 || c->ld_y % 8))
+    return FASTCLIP_ERR_UNSUPPORTED;
+  return FASTCLIP_OK;
+}
+// a stride that only some calls use
+static fastclip_status check_stride(const fastclip_linear_config& c, int64_t ld, int64_t width) {
+  if (ld < width) return FASTCLIP_ERR_SHAPE;
+  if (ld > ((int64_t)1 << 22) || (c.dtype == FASTCLIP_BF16 && ld % 8)) return FASTCLIP_ERR_UNSUPPORTED;
+  return FASTCLIP_OK;
+}
+// bf16 operands: 16-byte loads and stores everywhere; fp32: natural alignment
+static bool misaligned(const fastclip_linear_config& c, const void* p, int32_t type) {
+  return !aligned(p, c.dtype == FASTCLIP_BF16 ? 16 : size_of(type));
+}
+
+static LinearArgs linear_args(const fastclip_linear_config& c, int32_t pass) {
+  LinearArgs a;
+  memset(&a, 0, sizeof(a));
+  a.bf16 = c.dtype == FASTCLIP_BF16; a.out_bf16 = c.out_dtype == FASTCLIP_BF16;
+  a.act = c.activation;
+  if (pass == FASTCLIP_LINEAR_FORWARD) {
+    a.M = c.rows; a.N = c.d_out; a.K = c.d_in; a.ldp = c.ld_x; a.ldq = c.ld_w; a.ld_out = c.ld_y;
+  } else if (pass == FASTCLIP_LINEAR_BACKWARD_INPUT) {
+    a.M = c.rows; a.N = c.d_in; a.K = c.d_out; a.ldp = c.ld_y; a.ldq = c.ld_w; a.ld_out = c.ld_x;
+    a.q_by_depth = true;
+  } else {
+    a.M = c.d_out; a.N = c.d_in; a.K = c.rows; a.ldp = c.ld_y; a.ldq = c.ld_x; a.ld_out = c.ld_w;
+    a.p_by_depth = a.q_by_depth = true;
+    a.act = FASTCLIP_ACT_NONE;
+  }
+  return a;
+}
+static LinearPlan plan_of(const LinearArgs& a, int32_t pass) {
+  return plan_linear(a.M, a.N, a.K, a.bf16, a.p_by_depth, a.q_by_depth, pass == FASTCLIP_LINEAR_BACKWARD_WEIGHT);
+}
+
+static fastclip_status run_linear(LinearArgs& a, int32_t pass, void* workspace, size_t workspace_bytes, void* stream) {
+  hipStream_t s = (hipStream_t)stream;
+  if (a.M == 0) return FASTCLIP_OK;
+  if (a.K == 0) {
+    launch_linear_empty(a, s);
+    return launch_status();
+  }
+  const LinearPlan plan = plan_of(a, pass);
+  if (((a.M + plan.tile - 1) / plan.tile) * ((a.N + plan.tile - 1) / plan.tile) * plan.splits > (1 << 23))
+    return FASTCLIP_ERR_UNSUPPORTED;      // one launch
+  if (plan.bytes) {
+    if (!workspace) return FASTCLIP_ERR_NULL;
+    if (!aligned(workspace, 256)) return FASTCLIP_ERR_UNSUPPORTED;
+    if (workspace_bytes < plan.bytes) return FASTCLIP_ERR_WORKSPACE;
+    a.partial = (float*)workspace;
+  }
+  if (a.bf16) launch_linear_bf16(a, plan, s);
+  else launch_linear_f32(a, plan, s);
+  if (plan.splits > 1) launch_linear_join(a, plan, s);
+  return launch_status();
+}
+
+static fastclip_status check(const fastclip_adamw_config* c) {
+  if (!c) return FASTCLIP_ERR_NULL;
+  if (c->struct_size != sizeof(*c)) return FASTCLIP_ERR_SHAPE;
+  const float f[4] = {c->lr, c->beta1, c->beta2, c->eps};
+  for (float x : f)
+    if (not_finite(x) || x < 0.0f) return FASTCLIP_ERR_VALUE;
+  if ((c->state_bits != 32 && c->state_bits != 8) || !known_type(c->grad_dtype) || c->step < 1 || c->beta1 >= 1.0f ||
+      c->beta2 >= 1.0f)
+    return FASTCLIP_ERR_VALUE;
+  return FASTCLIP_OK;
+}
+static int64_t chunks_of(int64_t n) { return (n + kAdamwChunk - 1) / kAdamwChunk; }
+// -1: a tensor's size is negative, -2: more chunks than one launch takes
+static int64_t count_chunks(const fastclip_adamw_tensor* t, int64_t count) {
+  int64_t chunks = 0;
+  for (int64_t i = 0; i < count; ++i) {
+    if (t[i].n < 0) return -1;
+    if (t[i].n > ((int64_t)1 << 42)) return -2;
+    chunks += chunks_of(t[i].n);
+    if (chunks > 0x7fffffff) return -2;
+  }
+  return chunks;
+}
+static size_t entry_bytes(int64_t count) { return round_up(sizeof(AdamwEntry) * (size_t)count, 256); }
+
+}  // namespace fc
+
+extern "C" {
+
+fastclip_status fastclip_layer_norm_forward(const fastclip_layer_norm_config* cfg, const void* x, const float* weight,
+                                            const float* bias, void* y, float* mean, float* rstd, void* stream) {
+  const fastclip_status st = fc::check(cfg);
+  if (st != FASTCLIP_OK) return st;
+  if (cfg->rows == 0) return FASTCLIP_OK;
+  if (!x || !y) return FASTCLIP_ERR_NULL;
+  if (!fc::aligned(x, fc::size_of(cfg->x_dtype)) || !fc::aligned(y, fc::size_of(cfg->y_dtype)) || !fc::aligned(weight, 4) ||
+      !fc::aligned(bias, 4) || !fc::aligned(mean, 4) || !fc::aligned(rstd, 4))
+    return FASTCLIP_ERR_UNSUPPORTED;
+  fc::NormArgs a = fc::norm_args(*cfg);
+  a.x = x; a.weight = weight; a.bias = bias; a.out = y; a.mean = mean; a.rstd = rstd;
+  fc::launch_layer_norm_forward(a, (hipStream_t)stream);
+  return fc::launch_status();
+}
+
+size_t fastclip_layer_norm_backward_workspace_bytes(const fastclip_layer_norm_config* cfg) {
+  if (fc::check(cfg) != FASTCLIP_OK) return 0;
+  const int groups = fc::layer_norm_groups(cfg->rows, cfg->d);
+  return fc::round_up(sizeof(float) * 2 * (size_t)cfg->d * (size_t)(groups > 0 ? groups : 1), 256);
+}
+
+fastclip_status fastclip_layer_norm_backward(const fastclip_layer_norm_config* cfg, const void* x, const void* dy,
+                                             const float* mean, const float* rstd, const float* weight, void* dx,
+                                             float* dweight, float* dbias, void* workspace, size_t workspace_bytes,
+                                             void* stream) {
+  const fastclip_status st = fc::check(cfg);
+  if (st != FASTCLIP_OK) return st;
+  if (cfg->rows > 0 && (!x || !dy || !mean || !rstd || !dx)) return FASTCLIP_ERR_NULL;
+  if (!workspace) return FASTCLIP_ERR_NULL;
+  if (!fc::aligned(x, fc::size_of(cfg->x_dtype)) || !fc::aligned(dx, fc::size_of(cfg->x_dtype)) ||
+      !fc::aligned(dy, fc::size_of(cfg->y_dtype)) || !fc::aligned(mean, 4) || !fc::aligned(rstd, 4) || !fc::aligned(weight, 4) ||
+      !fc::aligned(dweight, 4) || !fc::aligned(dbias, 4) || !fc::aligned(workspace, 256))
+    return FASTCLIP_ERR_UNSUPPORTED;
+  if (workspace_bytes < fastclip_layer_norm_backward_workspace_bytes(cfg)) return FASTCLIP_ERR_WORKSPACE;
+  fc::NormArgs a = fc::norm_args(*cfg);
+  a.x = x; a.dy = dy; a.weight = weight; a.out = dx;
+  a.mean = const_cast<float*>(mean); a.rstd = const_cast<float*>(rstd);
+  a.partial = (float*)workspace;
+  fc::launch_layer_norm_backward(a, dweight, dbias, (hipStream_t)stream);
+  return fc::launch_status();
+}
+
+size_t fastclip_linear_workspace_bytes(const fastclip_linear_config* cfg, int32_t pass) {
+  if (fc::check(cfg, pass) != FASTCLIP_OK) return 0;
+  const fc::LinearArgs a = fc::linear_args(*cfg, pass);
+  return a.M == 0 || a.K == 0 ? 0 : fc::plan_of(a, pass).bytes;
+}
+
+fastclip_status fastclip_linear_forward(const fastclip_linear_config* cfg, const void* x, const void* w, const float* bias,
+                                        const void* residual, void* y, void* pre, void* workspace, size_t workspace_bytes,
+                                        void* stream) {
+  fastclip_status st = fc::check(cfg, FASTCLIP_LINEAR_FORWARD);
+  if (st == FASTCLIP_OK && residual) st = fc::check_stride(*cfg, cfg->ld_res, cfg->d_out);
+  if (st == FASTCLIP_OK && pre) st = fc::check_stride(*cfg, cfg->ld_pre, cfg->d_out);
+  if (st != FASTCLIP_OK) return st;
+  if (cfg->rows > 0 && (!x || !w || !y)) return FASTCLIP_ERR_NULL;
+  if (fc::misaligned(*cfg, x, cfg->dtype) || fc::misaligned(*cfg, w, cfg->dtype) || fc::misaligned(*cfg, y, cfg->out_dtype) ||
+      fc::misaligned(*cfg, residual, cfg->out_dtype) || fc::misaligned(*cfg, pre, cfg->dtype) || !fc::aligned(bias, 4))
+    return FASTCLIP_ERR_UNSUPPORTED;
+  fc::LinearArgs a = fc::linear_args(*cfg, FASTCLIP_LINEAR_FORWARD);
+  a.p = x; a.q = w; a.bias = bias; a.residual = residual; a.ld_res = cfg->ld_res; a.out = y; a.pre_out = pre;
+  a.ld_pre = cfg->ld_pre;
+  return fc::run_linear(a, FASTCLIP_LINEAR_FORWARD, workspace, workspace_bytes, stream);
+}
+
+fastclip_status fastclip_linear_backward_input(const fastclip_linear_config* cfg, const void* dy, const void* w, const void* pre,
+                                               void* dx, void* workspace, size_t workspace_bytes, void* stream) {
+  fastclip_status st = fc::check(cfg, FASTCLIP_LINEAR_BACKWARD_INPUT);
+  const bool slope = cfg && cfg->activation != FASTCLIP_ACT_NONE;
+  if (st == FASTCLIP_OK && slope) st = fc::check_stride(*cfg, cfg->ld_pre, cfg->d_in);
+  if (st != FASTCLIP_OK) return st;
+  if (cfg->rows > 0 && (!dy || !w || !dx || (slope && !pre))) return FASTCLIP_ERR_NULL;
+  if (fc::misaligned(*cfg, dy, cfg->dtype) || fc::misaligned(*cfg, w, cfg->dtype) || fc::misaligned(*cfg, dx, cfg->out_dtype) ||
+      (slope && fc::misaligned(*cfg, pre, cfg->dtype)))
+    return FASTCLIP_ERR_UNSUPPORTED;
+  fc::LinearArgs a = fc::linear_args(*cfg, FASTCLIP_LINEAR_BACKWARD_INPUT);
+  a.p = dy; a.q = w; a.out = dx; a.pre_in = slope ? pre : nullptr; a.ld_pre = cfg->ld_pre;
+  return fc::run_linear(a, FASTCLIP_LINEAR_BACKWARD_INPUT, workspace, workspace_bytes, stream);
+}
+
+fastclip_status fastclip_linear_backward_weight(const fastclip_linear_config* cfg, const void* dy, const void* x, void* dw,
+                                                float* dbias, void* workspace, size_t workspace_bytes, void* stream) {
+  const fastclip_status st = fc::check(cfg, FASTCLIP_LINEAR_BACKWARD_WEIGHT);
+  if (st != FASTCLIP_OK) return st;
+  if (!dw || (cfg->rows > 0 && (!dy || !x))) return FASTCLIP_ERR_NULL;
+  if (fc::misaligned(*cfg, dy, cfg->dtype) || fc::misaligned(*cfg, x, cfg->dtype) || fc::misaligned(*cfg, dw, cfg->out_dtype) ||
+      !fc::aligned(dbias, 4))
+    return FASTCLIP_ERR_UNSUPPORTED;
+  fc::LinearArgs a = fc::linear_args(*cfg, FASTCLIP_LINEAR_BACKWARD_WEIGHT);
+  a.p = dy; a.q = x; a.out = dw; a.dbias = dbias;
+  return fc::run_linear(a, FASTCLIP_LINEAR_BACKWARD_WEIGHT, workspace, workspace_bytes, stream);
+}
+
+size_t fastclip_adamw_table_bytes(const fastclip_adamw_tensor* tensors, int64_t count) {
+  if (count < 0 || count > 0x7fffffff || (count > 0 && !tensors)) return 0;
+  const int64_t chunks = fc::count_chunks(tensors, count);
+  return chunks < 0 ? 0 : fc::round_up(fc::entry_bytes(count) + sizeof(fc::AdamwChunk) * (size_t)chunks, 256);
+}
+
+fastclip_status fastclip_adamw_table_fill(const fastclip_adamw_config* cfg, const fastclip_adamw_tensor* tensors, int64_t count,
+                                          void* host_table, size_t bytes, fastclip_adamw_table* table) {
+  const fastclip_status st = fc::check(cfg);
+  if (st != FASTCLIP_OK) return st;
+  if (!table || (count > 0 && (!tensors || !host_table))) return FASTCLIP_ERR_NULL;
+  if (count < 0) return FASTCLIP_ERR_SHAPE;
+  if (count > 0x7fffffff) return FASTCLIP_ERR_UNSUPPORTED;
+  const int64_t chunks = fc::count_chunks(tensors, count);
+  if (chunks == -1) return FASTCLIP_ERR_SHAPE;
+  if (chunks < 0) return FASTCLIP_ERR_UNSUPPORTED;
+  const bool small = cfg->state_bits == 8;
+  const uintptr_t grad_size = fc::size_of(cfg->grad_dtype);
+  for (int64_t i = 0; i < count; ++i) {
+    const fastclip_adamw_tensor& t = tensors[i];
+    if (t.reserved != 0) return FASTCLIP_ERR_SHAPE;
+    if (fc::not_finite(t.weight_decay) || t.weight_decay < 0.0f) return FASTCLIP_ERR_VALUE;
+    if (t.n == 0) continue;
+    if (!t.param || !t.grad || !t.m || !t.v || (small && (!t.m_exp || !t.v_exp))) return FASTCLIP_ERR_NULL;
+    if (!fc::aligned(t.param, 4) || !fc::aligned(t.grad, grad_size) || !fc::aligned(t.param_bf16, 2) ||
+        (!small && (!fc::aligned(t.m, 4) || !fc::aligned(t.v, 4))))
+      return FASTCLIP_ERR_UNSUPPORTED;
+  }
+  if (bytes < fastclip_adamw_table_bytes(tensors, count)) return FASTCLIP_ERR_WORKSPACE;
+  if (bytes) memset(host_table, 0, bytes);
+  fc::AdamwEntry* e = (fc::AdamwEntry*)host_table;
+  fc::AdamwChunk* c = (fc::AdamwChunk*)((char*)host_table + fc::entry_bytes(count));
+  for (int64_t i = 0; i < count; ++i) {
+    const fastclip_adamw_tensor& t = tensors[i];
+    e[i].param = t.param; e[i].grad = t.grad; e[i].m = t.m; e[i].v = t.v; e[i].copy = (uint16_t*)t.param_bf16;
+    e[i].m_exp = t.m_exp; e[i].v_exp = t.v_exp; e[i].n = t.n; e[i].weight_decay = t.weight_decay;
+    e[i].wide = fc::aligned(t.param, 16) && fc::aligned(t.grad, 16) && fc::aligned(t.m, 16) && fc::aligned(t.v, 16) &&
+                fc::aligned(t.param_bf16, 16);
+    for (int64_t k = 0; k < fc::chunks_of(t.n); ++k) { c->tensor = (int32_t)i; c->chunk = (int32_t)k; ++c; }
+  }
+  table->struct_size = sizeof(*table);
+  table->state_bits = cfg->state_bits; table->grad_dtype = cfg->grad_dtype; table->reserved = 0;
+  table->tensors = count; table->chunks = chunks; table->device = nullptr;
+  return FASTCLIP_OK;
+}
+
+fastclip_status fastclip_adamw_step(const fastclip_adamw_config* cfg, const fastclip_adamw_table* table, void* stream) {
+  const fastclip_status st = fc::check(cfg);
+  if (st != FASTCLIP_OK) return st;
+  if (!table) return FASTCLIP_ERR_NULL;
+  if (table->struct_size != sizeof(*table) || table->tensors < 0 || table->chunks < 0 || table->chunks > 0x7fffffff)
+    return FASTCLIP_ERR_SHAPE;
+  if (table->state_bits != cfg->state_bits || table->grad_dtype != cfg->grad_dtype) return FASTCLIP_ERR_VALUE;
+  if (table->chunks == 0) return FASTCLIP_OK;
+  if (!table->device) return FASTCLIP_ERR_NULL;
+  if (!fc::aligned(table->device, 256)) return FASTCLIP_ERR_UNSUPPORTED;
+  fc::AdamwArgs a;
+  a.entries = (const fc::AdamwEntry*)table->device;
+  a.chunks = (const fc::AdamwChunk*)((const char*)table->device + fc::entry_bytes(table->tensors));
+  a.nchunks = table->chunks;
+  a.grad_bf16 = cfg->grad_dtype == FASTCLIP_BF16;
+  a.beta1 = cfg->beta1; a.beta2 = cfg->beta2; a.eps = cfg->eps; a.lr = cfg->lr;
+  // bias corrections 1 / (1 - beta^t), in double on the host
+  a.step_size = (float)((double)cfg->lr / (1.0 - pow((double)cfg->beta1, (double)cfg->step)));
+  a.corr2 = (float)(1.0 / (1.0 - pow((double)cfg->beta2, (double)cfg->step)));
+  a.seed = cfg->seed;
+  if (cfg->state_bits == 32) fc::launch_adamw_32(a, (hipStream_t)stream);
+  else fc::launch_adamw_8(a, (hipStream_t)stream);
+  return fc::launch_status();
+}
+
+fastclip_status fastclip_adamw_state_values(int32_t moment, const uint8_t* codes, const uint8_t* exponents, int64_t n,
+                                            float* out, void* stream) {
+  if (moment != FASTCLIP_ADAMW_FIRST && moment != FASTCLIP_ADAMW_SECOND) return FASTCLIP_ERR_VALUE;
+  if (n < 0) return FASTCLIP_ERR_SHAPE;
+  if (n == 0) return FASTCLIP_OK;
+  if (n > ((int64_t)1 << 42)) return FASTCLIP_ERR_UNSUPPORTED;
+  if (!codes || !exponents || !out) return FASTCLIP_ERR_NULL;
+  if (!fc::aligned(out, 4)) return FASTCLIP_ERR_UNSUPPORTED;
+  fc::launch_adamw_values(moment, codes, exponents, n, out, (hipStream_t)stream);
+  return fc::launch_status();
+}
+
+}  // extern "C"

@@ -31,6 +31,8 @@ def _asm_replacement(m):
     t = m.group(0)
     if "s_add_u32 m0" in t:                      # 16 bytes per lane into LDS at (uniform + IMM) + 16 lane
         return "emu_dma(uniform_base, lane_byte_off, lds_uniform + (uint32_t)IMM, 16);"
+    if "global_load_lds_dwordx4 %0, off" in t:   # ... from an address of the lane's own
+        return "emu_dma(lane_address, 0, lds_byte_addr, 16);"
     if "global_load_lds_dwordx4" in t:
         return "emu_dma(uniform_base, lane_byte_off, lds_byte_addr, 16);"
     if "global_load_lds_dword " in t:
@@ -141,6 +143,21 @@ def build(sanitizer: str = "-fsanitize=address") -> str:
     if r.returncode != 0:
         raise RuntimeError("link failed:\n" + r.stderr[-4000:])
     return EXE
+
+
+def build_operators(sanitizer: str = "-fsanitize=address") -> str:
+    """_build/emu/emu_operators: emu_operators.cpp with the same sources (build() shares its objects)."""
+    build(sanitizer)
+    exe = os.path.join(OUT, "emu_operators")
+    obj = os.path.join(OUT, "obj")
+    flags = ["-std=c++17", "-O1", "-g", "-fno-omit-frame-pointer", sanitizer, "-I", HERE, "-I", os.path.join(OUT, "gen"),
+             "-pthread", "-Wno-unused-value", "-Wno-ignored-attributes"]
+    objs = [os.path.join(obj, f) for f in sorted(os.listdir(obj)) if f.endswith(".o") and f != "emu_main.o"]
+    r = subprocess.run([host_compiler(), *flags, os.path.join(HERE, "emu_operators.cpp"), *objs, "-o", exe],
+                       capture_output=True, text=True)
+    if r.returncode != 0:
+        raise RuntimeError("link failed:\n" + r.stderr[-4000:])
+    return exe
 
 
 if __name__ == "__main__":

@@ -1,0 +1,79 @@
+// Calls one of the operators in front of the loss from the CPU build of the kernels' sources and writes its buffers back.
+// Every buffer is an exact-size allocation of its own (behind `skip` bytes of padding for a chosen alignment), so that
+// AddressSanitizer sees any access outside it.  Test infrastructure.
+//
+// Case file: int64 op, int64 count and int64 numbers, int64 count and float numbers, int64 count of buffers, each int64 bytes
+// (-1: NULL), int64 skip, the bytes.  Output: int32 status, then the bytes of every buffer that is not NULL.
+#define main emu_step_main
+#include "emu_main.cpp"
+#undef main
+
+static void* aligned_room(size_t bytes) {
+  void* p = nullptr;
+  return posix_memalign(&p, 256, bytes) ? nullptr : p;
+}
+
+int main(int argc, char** argv) {
+  if (argc != 3) return 2;
+  FILE* f = fopen(argv[1], "rb");
+  if (!f) return 2;
+  auto i64 = [&] { int64_t x; if (fread(&x, 8, 1, f) != 1) exit(2); return x; };
+  const int64_t op = i64();
+  std::vector<int64_t> n(i64());
+  for (auto& x : n) x = i64();
+  std::vector<float> r(i64());
+  for (auto& x : r) if (fread(&x, 4, 1, f) != 1) return 2;
+  const int64_t count = i64();
+  std::vector<char*> b;
+  std::vector<int64_t> bytes;
+  for (int64_t k = 0; k < count; ++k) {
+    const int64_t size = i64(), skip = i64();
+    bytes.push_back(size);
+    if (size < 0) { b.push_back(nullptr); continue; }
+    char* p = (char*)aligned_room((size_t)(size + skip + (size + skip ? 0 : 1)));
+    p += skip;
+    if (size && fread(p, 1, (size_t)size, f) != (size_t)size) return 2;
+    b.push_back(p);
+  }
+  fclose(f);
+  int32_t st = -1;
+  auto room = [&](size_t want) { return std::make_pair((void*)(want ? aligned_room(want) : nullptr), want); };
+  if (op == 0 || op == 1) {
+    fastclip_layer_norm_config c = {sizeof(c), (int32_t)n[0], (int32_t)n[1], r[0], n[2], n[3], n[4], n[5]};
+    if (op == 0) {
+      st = fastclip_layer_norm_forward(&c, b[0], (float*)b[1], (float*)b[2], b[3], (float*)b[4], (float*)b[5], nullptr);
+    } else {
+      const auto ws = room(fastclip_layer_norm_backward_workspace_bytes(&c));
+      memset(ws.first, 0xff, ws.second);
+      st = fastclip_layer_norm_backward(&c, b[0], b[1], (float*)b[2], (float*)b[3], (float*)b[4], b[5], (float*)b[6], (float*)b[7],
+                                        ws.first, ws.second, nullptr);
+    }
+  } else if (op <= 4) {
+    fastclip_linear_config c = {sizeof(c), (int32_t)n[0], (int32_t)n[1], (int32_t)n[2], n[3], n[4], n[5], n[6], n[7], n[8], n[9], n[10]};
+    const auto ws = room(fastclip_linear_workspace_bytes(&c, (int32_t)op - 2));
+    if (ws.first) memset(ws.first, 0xff, ws.second);
+    if (op == 2) st = fastclip_linear_forward(&c, b[0], b[1], (float*)b[2], b[3], b[4], b[5], ws.first, ws.second, nullptr);
+    if (op == 3) st = fastclip_linear_backward_input(&c, b[0], b[1], b[2], b[3], ws.first, ws.second, nullptr);
+    if (op == 4) st = fastclip_linear_backward_weight(&c, b[0], b[1], b[2], (float*)b[3], ws.first, ws.second, nullptr);
+  } else if (op == 5) {            // buffers: seven per tensor in the order of fastclip_adamw_tensor
+    fastclip_adamw_config c = {sizeof(c), (int32_t)n[0], (int32_t)n[1], (uint32_t)n[2], n[3], r[0], r[1], r[2], r[3]};
+    std::vector<fastclip_adamw_tensor> t;
+    for (size_t k = 0; 7 * k < b.size(); ++k)
+      t.push_back({(float*)b[7 * k], b[7 * k + 1], b[7 * k + 2], b[7 * k + 3], b[7 * k + 4], (uint8_t*)b[7 * k + 5],
+                   (uint8_t*)b[7 * k + 6], n[4 + k], r[4 + k], 0});
+    const auto tab = room(fastclip_adamw_table_bytes(t.data(), (int64_t)t.size()));
+    fastclip_adamw_table table;
+    st = fastclip_adamw_table_fill(&c, t.data(), (int64_t)t.size(), tab.first, tab.second, &table);
+    table.device = tab.first;
+    if (st == FASTCLIP_OK) st = fastclip_adamw_step(&c, &table, nullptr);
+  } else if (op == 6) {
+    st = fastclip_adamw_state_values((int32_t)n[0], (uint8_t*)b[0], (uint8_t*)b[1], n[1], (float*)b[2], nullptr);
+  }
+  f = fopen(argv[2], "wb");
+  if (!f) return 2;
+  fwrite(&st, 4, 1, f);
+  for (size_t k = 0; k < b.size(); ++k)
+    if (bytes[k] > 0) fwrite(b[k], 1, (size_t)bytes[k], f);
+  fclose(f);
+  return 0;
+}

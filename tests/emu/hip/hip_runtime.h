@@ -169,6 +169,43 @@ static inline emu_f32x16 __builtin_amdgcn_mfma_f32_32x32x16_bf16(emu_bf16x8 a, e
   w->bar.wait();
   return c;
 }
+// D = A B + C, 32 x 32 x 2 in fp32: lane (i, h) gives A[i][h] and B[h][i]; D as above
+static inline emu_f32x16 __builtin_amdgcn_mfma_f32_32x32x2f32(float a, float b, emu_f32x16 c, int, int, int) {
+  emu::Wave* w = emu::t_wave;
+  const int lane = emu::t_lane;
+  memcpy(w->buf[0][lane], &a, 4);
+  memcpy(w->buf[1][lane], &b, 4);
+  w->bar.wait();
+  const int n = lane & 31, h = lane >> 5;
+  for (int v = 0; v < 16; ++v) {
+    const int row = 8 * (v >> 2) + 4 * h + (v & 3);
+    for (int k = 0; k < 2; ++k) {
+      float x, y;
+      memcpy(&x, w->buf[0][row + 32 * k], 4);
+      memcpy(&y, w->buf[1][n + 32 * k], 4);
+      c[v] = fmaf(x, y, c[v]);
+    }
+  }
+  w->bar.wait();
+  return c;
+}
+// the upper half of the wave's a and the lower half of its b change places
+typedef uint32_t emu_u32x2 __attribute__((ext_vector_type(2)));
+static inline emu_u32x2 __builtin_amdgcn_permlane32_swap(uint32_t a, uint32_t b, bool, bool) {
+  emu::Wave* w = emu::t_wave;
+  const int lane = emu::t_lane;
+  memcpy(w->buf[0][lane], &a, 4);
+  memcpy(w->buf[1][lane], &b, 4);
+  w->bar.wait();
+  emu_u32x2 r;
+  uint32_t x, y;
+  memcpy(&x, w->buf[lane < 32 ? 0 : 1][lane & 31], 4);
+  memcpy(&y, w->buf[lane < 32 ? 0 : 1][lane | 32], 4);
+  r[0] = x;
+  r[1] = y;
+  w->bar.wait();
+  return r;
+}
 // D = A B + C, 16 x 16 x 4 in fp64: lane l gives A[l % 16][l / 16] and B[l / 16][l % 16]; D[4 v + l / 16][l % 16] in v
 typedef double emu_f64x4 __attribute__((ext_vector_type(4)));
 static inline emu_f64x4 __builtin_amdgcn_mfma_f64_16x16x4f64(double a, double b, emu_f64x4 c, int, int, int) {

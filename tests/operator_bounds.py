@@ -1,0 +1,89 @@
+"""Error bounds of the operators in front of the loss, for the tests on the CPU and on the GPU.
+
+Tolerances count roundings.  With u = 2^-24 (half a step of fp32) and h the half step of an output's type (bf16 2^-8): an
+output is |want| h for its own rounding, plus for a sum of K fp32 terms at most 2 K u times the sum of their magnitudes (the
+matrix cores may cut where others round: a whole step per addition), plus a few u for each product behind it.  The normal
+distribution function of the bf16 kernels is an approximation with an absolute error of 1.5e-7, taken as 4e-7 with the
+roundings around it."""
+from __future__ import annotations
+
+import numpy as np
+
+from oracle import operators_oracle as oo
+from paper_2407_01445_amd import binding as fc
+from paper_2407_01445_amd.workloads import round_to_bf16
+
+U = 2.0 ** -24
+HALF = {"f32": U, "bf16": 2.0 ** -8}
+KIND = {"f32": fc.F32, "bf16": fc.BF16}
+ACTS = {"": fc.ACT_NONE, "gelu": fc.ACT_GELU, "quick_gelu": fc.ACT_QUICK_GELU}
+
+
+def layer_norm_bounds(x, w, b, eps, y_type):
+    """(y, mean, rstd): a row's sums are trees of at most 32 additions deep; the centred values carry the mean's error."""
+    x = np.asarray(x, np.float64)
+    y, mean, rstd = oo.layer_norm(x, w, b, eps)
+    size = np.abs(x).mean(1)
+    mean_err = 40 * U * size
+    rstd_rel = 40 * U + (mean_err * rstd) ** 2
+    w_abs = np.ones(x.shape[1]) if w is None else np.abs(w)
+    y_err = ((mean_err + 2 * U * np.abs(mean))[:, None] * rstd[:, None] +
+             np.abs(x - mean[:, None]) * rstd[:, None] * (rstd_rel[:, None] + 8 * U)) * w_abs
+    return y_err + np.abs(y) * (HALF[y_type] + 4 * U) + 1e-37, mean_err + 1e-37, rstd * (rstd_rel + 4 * U)
+
+
+def layer_norm_grad_bounds(x, dy, mean, rstd, w, x_type):
+    x, dy = np.asarray(x, np.float64), np.asarray(dy, np.float64)
+    dx, dw, db = oo.layer_norm_grad(x, dy, mean, rstd, w)
+    rows, d = x.shape
+    xh = np.abs(x - mean[:, None]) * rstd[:, None]
+    xh_err = 4 * U * xh + 2 * U * np.abs(x) * rstd[:, None]
+    q = np.abs(dy) * (1 if w is None else np.abs(w))
+    s1, s2 = q.mean(1, keepdims=True), (q * xh).mean(1, keepdims=True)
+    s2_err = 40 * U * s2 + (q * xh_err).mean(1, keepdims=True)
+    dx_err = rstd[:, None] * (8 * U * (q + s1 + xh * s2) + 40 * U * s1 + xh * s2_err + xh_err * s2)
+    deep = 2 * rows * U
+    return (dx_err + np.abs(dx) * HALF[x_type] + 1e-37, deep * (np.abs(dy) * xh).sum(0) + (np.abs(dy) * xh_err).sum(0) + 1e-37,
+            deep * np.abs(dy).sum(0) + 1e-37)
+
+
+def linear_bounds(x, w, bias, act, residual, out_type, type):
+    y, z = oo.linear(x, w, bias, act, residual)
+    K = x.shape[1]
+    z_err = 2 * K * U * (np.abs(x).astype(np.float64) @ np.abs(w).astype(np.float64).T) + 2 * U * np.abs(z)
+    y_err = 1.13 * z_err + (4e-7 * np.abs(z) if act else 0) + 4 * U * (0 if residual is None else np.abs(residual))
+    return y_err + np.abs(y) * (HALF[out_type] + 2 * U) + 1e-37, z_err + np.abs(z) * HALF[type] + 1e-37
+
+
+def linear_grad_input_bound(dy, w, pre, act, out_type):
+    dx = oo.linear_grad_input(dy, w, pre, act)
+    raw = np.abs(oo.linear_grad_input(dy, w))
+    K = dy.shape[1]
+    err = 2 * K * U * (np.abs(dy).astype(np.float64) @ np.abs(w).astype(np.float64)) * 1.13 + (1.5e-6 * raw if act else 0)
+    return err + np.abs(dx) * (HALF[out_type] + 2 * U) + 1e-37
+
+
+def linear_grad_weight_bounds(dy, x, out_type):
+    dw, db = oo.linear_grad_weight(dy, x)
+    K = dy.shape[0]
+    dy, x = np.abs(dy).astype(np.float64), np.abs(x).astype(np.float64)
+    return (2 * K * U * (dy.T @ x) + np.abs(dw) * HALF[out_type] + 1e-37, 2 * K * U * dy.sum(0) + 1e-37)
+
+
+def within(got, want, bound, what):
+    got, want = np.asarray(got, np.float64), np.asarray(want, np.float64)
+    off = np.abs(got - want) - bound
+    assert np.all(off <= 0), (what, float(np.max(off)), int(np.argmax(off)), float(np.max(np.abs(got - want))))
+
+
+def held(x, kind):
+    """fp32 values as a type holds them."""
+    return round_to_bf16(x) if kind == "bf16" else np.ascontiguousarray(x, np.float32)
+
+
+def matrices(rng, rows, d_in, d_out, type):
+    """(x, w, dy) of a layer."""
+    x = held(rng.normal(0, 1, (rows, d_in)).astype(np.float32), type)
+    w = held(rng.normal(0, d_in ** -0.5, (d_out, d_in)).astype(np.float32), type)
+    dy = held(rng.normal(0, 1, (rows, d_out)).astype(np.float32), type)
+    return x, w, dy

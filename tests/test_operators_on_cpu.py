@@ -1,0 +1,519 @@
+"""The operators in front of the loss without a GPU: argument checks of the entry points, the oracle against differences and
+closed forms, and the kernels' own sources in the host build of tests/emu under AddressSanitizer against the oracle.  operator_bounds.py has the error bounds."""
+from __future__ import annotations
+
+import ctypes as C
+import os
+import subprocess
+import sys
+
+import numpy as np
+import pytest
+
+ROOT = os.path.dirname(os.path.dirname(os.path.abspath(__file__)))
+sys.path.insert(0, os.path.join(ROOT, "tests", "emu"))
+import build_emu  # noqa: E402
+
+from operator_bounds import (ACTS, KIND, U, held, layer_norm_bounds, layer_norm_grad_bounds, linear_bounds,  # noqa: E402
+                             linear_grad_input_bound, linear_grad_weight_bounds, matrices, within)
+from oracle import operators_oracle as oo  # noqa: E402
+from paper_2407_01445_amd import binding as fc  # noqa: E402
+from paper_2407_01445_amd.workloads import round_to_bf16  # noqa: E402
+
+# ---- refusals -----------------------------------------------------------------------------------------------------------
+
+P = 0x10000            # an aligned address; nothing is dereferenced on the paths tested here
+
+
+def ln_cfg(**over):
+    kw = dict(rows=16, d=64, x_dtype=fc.F32, y_dtype=fc.BF16, eps=1e-5)
+    kw.update(over)
+    return fc.make_layer_norm_config(**kw)
+
+
+def lin_cfg(**over):
+    kw = dict(rows=16, d_in=64, d_out=128, dtype=fc.BF16)
+    kw.update(over)
+    return fc.make_linear_config(**kw)
+
+
+@pytest.mark.parametrize("over,status", [
+    (dict(rows=-1), fc.ERR_SHAPE), (dict(d=0), fc.ERR_SHAPE), (dict(ld_x=63), fc.ERR_SHAPE), (dict(ld_y=63), fc.ERR_SHAPE),
+    (dict(x_dtype=2), fc.ERR_VALUE), (dict(y_dtype=-1), fc.ERR_VALUE), (dict(eps=-1e-9), fc.ERR_VALUE),
+    (dict(eps=float("nan")), fc.ERR_VALUE), (dict(rows=1 << 31), fc.ERR_UNSUPPORTED), (dict(ld_x=1 << 31), fc.ERR_UNSUPPORTED)])
+def test_layer_norm_refuses_bad_configurations(over, status):
+    cfg = ln_cfg(**over)
+    assert fc.fastclip_layer_norm_forward(cfg, P, P, P, P, P, P, stream=0, check=False) == status
+    assert fc.fastclip_layer_norm_backward(cfg, P, P, P, P, P, P, P, P, P, 1 << 40, stream=0, check=False) == status
+    assert fc.fastclip_layer_norm_backward_workspace_bytes(cfg) == 0
+    cfg.struct_size += 4
+    assert fc.fastclip_layer_norm_forward(cfg, P, P, P, P, P, P, stream=0, check=False) == fc.ERR_SHAPE
+
+
+def test_layer_norm_refuses_bad_pointers():
+    cfg = ln_cfg()
+    need = fc.fastclip_layer_norm_backward_workspace_bytes(cfg)
+    assert need >= 2 * 64 * 4 and need % 256 == 0
+    forward = lambda *p: fc.fastclip_layer_norm_forward(cfg, *p, stream=0, check=False)
+    assert forward(None, P, P, P, P, P) == fc.ERR_NULL and forward(P, P, P, None, P, P) == fc.ERR_NULL
+    assert forward(P + 2, P, P, P, P, P) == fc.ERR_UNSUPPORTED and forward(P, P, P, P + 1, P, P) == fc.ERR_UNSUPPORTED
+    assert forward(P, P + 1, P, P, P, P) == fc.ERR_UNSUPPORTED and forward(P, P, P, P, P, P + 2) == fc.ERR_UNSUPPORTED
+    good = [P] * 9
+    for i in (0, 1, 2, 3, 5, 8):
+        bad = list(good)
+        bad[i] = None
+        assert fc.fastclip_layer_norm_backward(cfg, *bad, need, stream=0, check=False) == fc.ERR_NULL
+    back = lambda p, n: fc.fastclip_layer_norm_backward(cfg, *p, n, stream=0, check=False)
+    assert back(good, need - 1) == fc.ERR_WORKSPACE
+    assert back(good[:8] + [P + 128], need) == fc.ERR_UNSUPPORTED
+    empty = ln_cfg(rows=0)
+    assert fc.fastclip_layer_norm_forward(empty, None, None, None, None, stream=0, check=False) == fc.OK
+
+
+@pytest.mark.parametrize("over,status", [
+    (dict(rows=-1), fc.ERR_SHAPE), (dict(d_in=0), fc.ERR_SHAPE), (dict(d_out=0), fc.ERR_SHAPE), (dict(ld_x=56), fc.ERR_SHAPE),
+    (dict(ld_w=56), fc.ERR_SHAPE), (dict(ld_y=120), fc.ERR_SHAPE), (dict(dtype=2), fc.ERR_VALUE), (dict(out_dtype=5), fc.ERR_VALUE),
+    (dict(activation=3), fc.ERR_VALUE), (dict(activation=-1), fc.ERR_VALUE), (dict(d_in=60), fc.ERR_UNSUPPORTED),
+    (dict(d_out=132), fc.ERR_UNSUPPORTED), (dict(ld_x=68), fc.ERR_UNSUPPORTED), (dict(ld_w=100), fc.ERR_UNSUPPORTED),
+    (dict(ld_y=132), fc.ERR_UNSUPPORTED), (dict(rows=(1 << 30) + 1), fc.ERR_UNSUPPORTED),
+    (dict(ld_x=(1 << 22) + 8), fc.ERR_UNSUPPORTED)])
+def test_linear_refuses_bad_configurations(over, status):
+    cfg = lin_cfg(**over)
+    assert fc.fastclip_linear_forward(cfg, P, P, P, P, P, P, P, 1 << 40, stream=0, check=False) == status
+    assert fc.fastclip_linear_backward_input(cfg, P, P, P, P, P, 1 << 40, stream=0, check=False) == status
+    assert fc.fastclip_linear_backward_weight(cfg, P, P, P, P, P, 1 << 40, stream=0, check=False) == status
+    assert all(fc.fastclip_linear_workspace_bytes(cfg, which) == 0 for which in range(3))
+
+
+def test_linear_refuses_bad_pointers_and_strides():
+    cfg = lin_cfg(activation=fc.ACT_GELU, ld_pre=128, ld_res=128)
+    forward = lambda c, *p: fc.fastclip_linear_forward(c, *p, P, 1 << 40, stream=0, check=False)
+    for i in (0, 1, 4):
+        bad = [P] * 6
+        bad[i] = None
+        assert forward(cfg, *bad) == fc.ERR_NULL
+    for i in (0, 1, 3, 4, 5):
+        bad = [P] * 6
+        bad[i] = P + 8
+        assert forward(cfg, *bad) == fc.ERR_UNSUPPORTED
+    assert forward(cfg, P, P, P + 2, P, P, P) == fc.ERR_UNSUPPORTED
+    assert forward(lin_cfg(ld_res=120), P, P, P, P, P, None) == fc.ERR_SHAPE
+    assert forward(lin_cfg(ld_pre=120), P, P, P, None, P, P) == fc.ERR_SHAPE
+    assert forward(lin_cfg(ld_res=132), P, P, P, P, P, None) == fc.ERR_UNSUPPORTED
+    back = lambda c, *p: fc.fastclip_linear_backward_input(c, *p, P, 1 << 40, stream=0, check=False)
+    assert back(cfg, P, P, None, P) == fc.ERR_NULL and back(cfg, P, P, P + 8, P) == fc.ERR_UNSUPPORTED
+    assert back(lin_cfg(activation=fc.ACT_GELU, ld_pre=56), P, P, P, P) == fc.ERR_SHAPE
+    assert fc.fastclip_linear_backward_weight(cfg, P, P, None, P, P, 1 << 40, stream=0, check=False) == fc.ERR_NULL
+    assert fc.fastclip_linear_workspace_bytes(cfg, 3) == 0
+    # a pass that splits its depth asks for its workspace
+    deep = lin_cfg(rows=16384, d_in=64, d_out=64)
+    need = fc.fastclip_linear_workspace_bytes(deep, fc.LINEAR_BACKWARD_WEIGHT)
+    assert need > 0 and need % 256 == 0
+    weight = lambda ws, n: fc.fastclip_linear_backward_weight(deep, P, P, P, None, ws, n, stream=0, check=False)
+    assert weight(None, need) == fc.ERR_NULL and weight(P, need - 1) == fc.ERR_WORKSPACE
+    assert weight(P + 128, need) == fc.ERR_UNSUPPORTED
+    # outputs beyond one launch
+    wide = lin_cfg(rows=1 << 30, d_in=8, d_out=1 << 22, ld_y=1 << 22)
+    assert fc.fastclip_linear_forward(wide, P, P, None, None, P, None, P, 1 << 40, stream=0, check=False) == fc.ERR_UNSUPPORTED
+    nothing = lin_cfg(rows=0)
+    assert fc.fastclip_linear_forward(nothing, None, None, None, None, None, stream=0, check=False) == fc.OK
+
+
+def adamw_cfg(**over):
+    kw = dict(state_bits=32, grad_dtype=fc.F32, step=1, lr=1e-3, beta1=0.9, beta2=0.98)
+    kw.update(over)
+    return fc.make_adamw_config(**kw)
+
+
+def fill(cfg, tensors):
+    lib = fc.load()
+    array = (fc.fastclip_adamw_tensor * max(1, len(tensors)))(*tensors)
+    nbytes = int(lib.fastclip_adamw_table_bytes(array, len(tensors)))
+    host = (C.c_char * max(1, nbytes))()
+    table = fc.fastclip_adamw_table()
+    st = int(lib.fastclip_adamw_table_fill(C.byref(cfg), array, len(tensors), C.cast(host, C.c_void_p), nbytes, C.byref(table)))
+    return st, table, nbytes
+
+
+def entry(n=1000, **over):
+    kw = dict(param=P, grad=P, m=P, v=P, param_bf16=P, m_exp=P, v_exp=P, n=n, weight_decay=0.1, reserved=0)
+    kw.update(over)
+    return fc.fastclip_adamw_tensor(**kw)
+
+
+@pytest.mark.parametrize("over", [dict(state_bits=16), dict(grad_dtype=2), dict(step=0), dict(lr=-1.0), dict(beta1=1.0),
+                                  dict(beta2=1.0), dict(beta1=-0.1), dict(eps=-1e-8), dict(lr=float("inf")), dict(eps=float("nan"))])
+def test_adamw_refuses_bad_configurations(over):
+    st, table, _ = fill(adamw_cfg(), [entry()])
+    assert st == fc.OK
+    table.device = P
+    assert fill(adamw_cfg(**over), [entry()])[0] == fc.ERR_VALUE
+    assert fc.fastclip_adamw_step(adamw_cfg(**over), table, stream=0, check=False) == fc.ERR_VALUE
+
+
+def test_adamw_tables():
+    cfg = adamw_cfg()
+    st, table, nbytes = fill(cfg, [entry(1), entry(0, param=None), entry(4096), entry(4097)])
+    assert st == fc.OK and (table.tensors, table.chunks) == (4, 4) and nbytes % 256 == 0 and table.device is None
+    assert fill(cfg, [entry(-1)])[0] in (fc.ERR_SHAPE,)
+    for name in ("param", "grad", "m", "v"):
+        assert fill(cfg, [entry(), entry(**{name: None})])[0] == fc.ERR_NULL
+        assert fill(cfg, [entry(**{name: P + 2})])[0] == fc.ERR_UNSUPPORTED
+    assert fill(cfg, [entry(m_exp=None, v_exp=None, param_bf16=None)])[0] == fc.OK
+    assert fill(adamw_cfg(state_bits=8), [entry(m_exp=None)])[0] == fc.ERR_NULL
+    assert fill(adamw_cfg(state_bits=8), [entry(m=P + 1, v=P + 3)])[0] == fc.OK
+    assert fill(cfg, [entry(weight_decay=-0.1)])[0] == fc.ERR_VALUE
+    assert fill(cfg, [entry(weight_decay=float("nan"))])[0] == fc.ERR_VALUE
+    assert fill(cfg, [entry(reserved=1)])[0] == fc.ERR_SHAPE
+    assert fill(cfg, [entry(1 << 43)])[0] == fc.ERR_UNSUPPORTED
+    # steps
+    step = lambda c: fc.fastclip_adamw_step(c, table, stream=0, check=False)
+    assert step(cfg) == fc.ERR_NULL                                  # not on the device yet
+    table.device = P + 64
+    assert step(cfg) == fc.ERR_UNSUPPORTED
+    table.device = P
+    assert step(adamw_cfg(state_bits=8)) == fc.ERR_VALUE and step(adamw_cfg(grad_dtype=fc.BF16)) == fc.ERR_VALUE
+    table.struct_size = 0
+    assert step(cfg) == fc.ERR_SHAPE
+    st, empty, _ = fill(cfg, [])
+    assert st == fc.OK and empty.chunks == 0
+    assert fc.fastclip_adamw_step(cfg, empty, stream=0, check=False) == fc.OK
+    values = lambda *a: fc.fastclip_adamw_state_values(*a, stream=0, check=False)
+    assert values(0, P, P, 5, P) == fc.ERR_VALUE and values(1, P, P, -1, P) == fc.ERR_SHAPE
+    assert values(1, None, P, 5, P) == fc.ERR_NULL and values(2, P, P, 5, P + 2) == fc.ERR_UNSUPPORTED
+    assert values(1, None, None, 0, None) == fc.OK
+
+
+def test_adamw_tensors_of_the_wrong_kind():
+    import torch
+    f, b, u = torch.zeros(300), torch.zeros(300, dtype=torch.bfloat16), torch.zeros(300, dtype=torch.uint8)
+    with pytest.raises(ValueError):
+        fc.make_adamw_tensor(param=f, grad=f[:299], m=f, v=f)
+    with pytest.raises(ValueError):
+        fc.make_adamw_tensor(param=f, grad=torch.zeros(600)[::2], m=f, v=f)
+    with pytest.raises(ValueError):
+        fc.make_adamw_tensor(param=f, grad=f, m=u, v=u, m_exp=u[:1], v_exp=u[:2])
+    with pytest.raises(TypeError):
+        fc.make_adamw_tensor(param=f, grad=f, m=f, v=f)               # host tensors
+    t = entry()
+    t._types = ("torch.float32",) * 4 + (None,) * 3
+    t._keepalive = [b]
+    with pytest.raises(TypeError):
+        fc.make_adamw_table(adamw_cfg(grad_dtype=fc.BF16), [t])
+    with pytest.raises(TypeError):
+        fc.make_adamw_table(adamw_cfg(state_bits=8), [t])
+
+
+# ---- the oracle ---------------------------------------------------------------------------------------------------------
+
+def differences(f, x, up, steps=1e-6):
+    """Gradient of sum(up * f(x)) by central differences."""
+    x = np.array(x, np.float64)
+    out = np.zeros_like(x)
+    for i in np.ndindex(*x.shape):
+        old = x[i]
+        x[i] = old + steps
+        hi = np.sum(up * f(x))
+        x[i] = old - steps
+        out[i] = (hi - np.sum(up * f(x))) / (2 * steps)
+        x[i] = old
+    return out
+
+
+def test_oracle_layer_norm_gradient_against_differences():
+    rng = np.random.default_rng(0)
+    x, w, b, up = rng.normal(1, 2, (3, 7)), rng.normal(1, 0.3, 7), rng.normal(0, 1, 7), rng.normal(0, 1, (3, 7))
+    _, mean, rstd = oo.layer_norm(x, w, b, 1e-3)
+    dx, dw, db = oo.layer_norm_grad(x, up, mean, rstd, w)
+    np.testing.assert_allclose(dx, differences(lambda t: oo.layer_norm(t, w, b, 1e-3)[0], x, up), atol=1e-7)
+    np.testing.assert_allclose(dw, differences(lambda t: oo.layer_norm(x, t, b, 1e-3)[0], w, up), atol=1e-7)
+    np.testing.assert_allclose(db, differences(lambda t: oo.layer_norm(x, w, t, 1e-3)[0], b, up), atol=1e-7)
+
+
+@pytest.mark.parametrize("act", ["", "gelu", "quick_gelu"])
+def test_oracle_linear_gradients_against_differences(act):
+    rng = np.random.default_rng(1)
+    z0, w, b, up = rng.normal(0, 1.5, (4, 6)), rng.normal(0, 0.5, (5, 6)), rng.normal(0, 1, 5), rng.normal(0, 1, (4, 5))
+    f = lambda z, w_=w, b_=b: oo.linear(oo.activation(z, act), w_, b_)[0]
+    np.testing.assert_allclose(oo.linear_grad_input(up, w, z0, act), differences(f, z0, up), atol=1e-7)
+    dw, db = oo.linear_grad_weight(up, oo.activation(z0, act))
+    np.testing.assert_allclose(dw, differences(lambda t: f(z0, t), w, up), atol=1e-7)
+    np.testing.assert_allclose(db, differences(lambda t: f(z0, w, t), b, up), atol=1e-7)
+
+
+def test_oracle_eight_bit_moments_round_to_neighbours_and_keep_the_mean():
+    rng = np.random.default_rng(2)
+    x = rng.normal(0, 1, 4096) * np.exp(rng.normal(0, 2, 4096))
+    for second in (False, True):
+        y = np.abs(x) if second else x
+        total = np.zeros_like(y)
+        for s in range(64):
+            c, e = oo.encode(y, oo.random_halves(s, 3, y.size)[int(second)], second)
+            got = oo.decode(c, e, second)
+            lo, _ = oo.encode(y, np.zeros(y.size, np.int64), second)
+            hi, _ = oo.encode(y, np.full(y.size, 65535), second)
+            assert np.all((c == lo) | (c == hi) | (second & (c == 1)))
+            total += got
+        # mean over 64 draws: a remainder's standard deviation is at most half a step, steps are at most 1/8 of a value
+        # above the smallest octave
+        big = np.abs(y) > np.repeat(np.abs(y).reshape(-1, 256).max(1), 256) * 2.0 ** -12
+        assert np.max(np.abs(total / 64 - y)[big] / np.abs(y)[big]) <= 6 * 0.5 / 8 / 8
+
+
+# ---- the kernels' sources on the host --------------------------------------------------------------------------------------
+
+SANITIZER = os.environ.get("FASTCLIP_EMU_SANITIZER", "address")
+
+
+@pytest.fixture(scope="module")
+def emu():
+    if build_emu.host_compiler() is None:
+        pytest.skip("no host clang++ to build the emulation with")
+    return build_emu.build_operators("-fsanitize=" + SANITIZER)
+
+
+def call(exe, tmp_path, op, numbers, floats, buffers):
+    """buffers: None or (array, skip): skip bytes in front of it inside a 256-byte aligned allocation."""
+    fin, fout = str(tmp_path / "op.in"), str(tmp_path / "op.out")
+    with open(fin, "wb") as f:
+        np.array([op, len(numbers), *numbers], np.int64).tofile(f)
+        np.array([len(floats)], np.int64).tofile(f)
+        np.array(floats, np.float32).tofile(f)
+        np.array([len(buffers)], np.int64).tofile(f)
+        for b in buffers:
+            if b is None:
+                np.array([-1, 0], np.int64).tofile(f)
+            else:
+                np.array([b[0].nbytes, b[1]], np.int64).tofile(f)
+                b[0].tofile(f)
+    env = dict(os.environ, ASAN_OPTIONS="detect_leaks=0", TSAN_OPTIONS="report_thread_leaks=0")
+    r = subprocess.run([exe, fin, fout], capture_output=True, text=True, timeout=600, env=env)
+    assert r.returncode == 0 and "Sanitizer" not in r.stderr, "the CPU build of the kernels failed\n" + r.stderr[:6000]
+    raw = open(fout, "rb").read()
+    assert np.frombuffer(raw[:4], np.int32)[0] == fc.OK
+    out, at = [], 4
+    for b in buffers:
+        if b is None:
+            out.append(None)
+            continue
+        out.append(np.frombuffer(raw[at:at + b[0].nbytes], b[0].dtype).reshape(b[0].shape).copy())
+        at += b[0].nbytes
+    assert at == len(raw)
+    return out
+
+
+def rows_of(x, ld, kind):
+    """The memory of a matrix of row stride ld that ends with its last row's last element, NaN between the rows."""
+    rows, d = x.shape
+    if rows == 0:
+        return np.zeros(0, np.float32 if kind == "f32" else np.uint16)
+    full = np.full((rows, ld), np.nan, np.float32)
+    full[:, :d] = x
+    flat = full.reshape(-1)[:(rows - 1) * ld + d]
+    return (flat.view(np.uint32) >> 16).astype(np.uint16) if kind == "bf16" else flat.copy()
+
+
+def empty_rows(rows, d, ld, kind):
+    return rows_of(np.full((rows, d), np.nan, np.float32), ld, kind)
+
+
+def values_of(flat, rows, d, ld, kind):
+    x = (flat.astype(np.uint32) << 16).view(np.float32) if kind == "bf16" else flat
+    full = np.full(rows * ld, np.nan, np.float32)
+    full[:x.size] = x
+    full = full.reshape(rows, ld)
+    assert np.all(np.isnan(full[:, d:])), "a store between the rows"
+    return full[:, :d].astype(np.float64)
+
+
+LN_CASES = [       # rows, d, ld_x, ld_y, x, y, skip: wide and single loads, a wavefront or a workgroup a row, rows of one element
+    (5, 64, 64, 64, "bf16", "bf16", 0), (9, 520, 528, 520, "f32", "bf16", 0), (3, 19, 23, 19, "f32", "f32", 4),
+    (6, 1, 1, 1, "bf16", "f32", 0), (2, 1030, 1031, 1033, "f32", "f32", 0), (3, 1032, 1040, 1032, "bf16", "bf16", 0),
+    (2, 2056, 2056, 2056, "f32", "bf16", 0), (3, 4100, 4100, 4101, "bf16", "f32", 0), (1, 300, 300, 300, "bf16", "bf16", 2)]
+
+
+@pytest.mark.parametrize("rows,d,ld_x,ld_y,xt,yt,skip", LN_CASES)
+def test_layer_norm_sources_on_the_host(emu, tmp_path, rows, d, ld_x, ld_y, xt, yt, skip):
+    rng = np.random.default_rng(d)
+    x = held(rng.normal(3, 2, (rows, d)).astype(np.float32), xt)
+    w, b = rng.normal(1, 0.3, d).astype(np.float32), rng.normal(0, 0.3, d).astype(np.float32)
+    eps = np.float32(1e-5)
+    numbers = [KIND[xt], KIND[yt], rows, d, ld_x, ld_y]
+    nan = np.full(rows, np.nan, np.float32)
+    out = call(emu, tmp_path, 0, numbers, [eps], [(rows_of(x, ld_x, xt), skip), (w, 0), (b, 0),
+                                                  (empty_rows(rows, d, ld_y, yt), 0), (nan, 0), (nan, 0)])
+    want, bound = oo.layer_norm(x, w, b, float(eps)), layer_norm_bounds(x, w, b, float(eps), yt)
+    within(values_of(out[3], rows, d, ld_y, yt), want[0], bound[0], "y")
+    within(out[4], want[1], bound[1], "mean")
+    within(out[5], want[2], bound[2], "rstd")
+    dy = held(rng.normal(0, 1, (rows, d)).astype(np.float32), yt)
+    mean, rstd = want[1].astype(np.float32), want[2].astype(np.float32)
+    cols = np.full(d, np.nan, np.float32)
+    out = call(emu, tmp_path, 1, numbers, [eps], [(rows_of(x, ld_x, xt), skip), (rows_of(dy, ld_y, yt), 0), (mean, 0), (rstd, 0),
+                                                  (w, 0), (empty_rows(rows, d, ld_x, xt), 0), (cols, 0), (cols, 0)])
+    want = oo.layer_norm_grad(x, dy, mean, rstd, w)
+    bound = layer_norm_grad_bounds(x, dy, mean, rstd, w, xt)
+    within(values_of(out[5], rows, d, ld_x, xt), want[0], bound[0], "dx")
+    within(out[6], want[1], bound[1], "dweight")
+    within(out[7], want[2], bound[2], "dbias")
+
+
+def test_layer_norm_without_affine_and_without_rows(emu, tmp_path):
+    rng = np.random.default_rng(5)
+    x = rng.normal(0, 1, (4, 40)).astype(np.float32)
+    out = call(emu, tmp_path, 0, [fc.F32, fc.F32, 4, 40, 40, 40], [1e-6],
+               [(x, 0), None, None, (np.zeros_like(x), 0), None, None])
+    within(out[3], oo.layer_norm(x, None, None, float(np.float32(1e-6)))[0],
+           layer_norm_bounds(x, None, None, float(np.float32(1e-6)), "f32")[0], "y")
+    none = np.zeros((0, 40), np.float32)
+    out = call(emu, tmp_path, 1, [fc.F32, fc.F32, 0, 40, 40, 40], [1e-6],
+               [(none, 0), (none, 0), (none, 0), (none, 0), None, (none, 0), (np.ones(40, np.float32), 0), None])
+    assert np.all(out[6] == 0)
+
+
+LIN_CASES = [      # rows, d_in, d_out, type, out, act, bias, residual, keep, pad
+    (3, 8, 8, "bf16", "bf16", "", False, False, False, 0), (70, 72, 136, "bf16", "bf16", "gelu", True, True, True, 8),
+    (33, 200, 64, "bf16", "f32", "quick_gelu", True, False, True, 0), (1, 520, 40, "bf16", "f32", "gelu", True, True, False, 0),
+    (5, 7, 3, "f32", "f32", "gelu", True, True, True, 5), (65, 33, 70, "f32", "f32", "", True, False, False, 0),
+    (40, 132, 64, "f32", "bf16", "quick_gelu", False, True, True, 4), (1, 1, 1, "f32", "f32", "", True, False, False, 0)]
+
+
+@pytest.mark.parametrize("rows,d_in,d_out,type,out_type,act,bias,residual,keep,pad", LIN_CASES)
+def test_linear_sources_on_the_host(emu, tmp_path, rows, d_in, d_out, type, out_type, act, bias, residual, keep, pad):
+    rng = np.random.default_rng(rows + d_in)
+    x, w, dy = matrices(rng, rows, d_in, d_out, type)
+    li, lo = d_in + pad, d_out + pad
+    b = rng.normal(0, 1, d_out).astype(np.float32) if bias else None
+    res = held(rng.normal(0, 1, (rows, d_out)).astype(np.float32), out_type) if residual else None
+    numbers = [KIND[type], KIND[out_type], ACTS[act], rows, d_in, d_out, li, li, lo, lo, lo]
+    buf = lambda a, ld, kind: (rows_of(a, ld, kind), 0)
+    out = call(emu, tmp_path, 2, numbers, [], [
+        buf(x, li, type), buf(w, li, type), None if b is None else (b, 0), None if res is None else buf(res, lo, out_type),
+        (empty_rows(rows, d_out, lo, out_type), 0), (empty_rows(rows, d_out, lo, type), 0) if keep else None])
+    want, bound = oo.linear(x, w, b, act, res), linear_bounds(x, w, b, act, res, out_type, type)
+    within(values_of(out[4], rows, d_out, lo, out_type), want[0], bound[0], "y")
+    if keep:
+        within(values_of(out[5], rows, d_out, lo, type), want[1], bound[1], "pre")
+    # the input's gradient through the activation in front
+    pre = held(rng.normal(0, 2, (rows, d_in)).astype(np.float32), type) if act else None
+    numbers[9] = li
+    out = call(emu, tmp_path, 3, numbers, [], [buf(dy, lo, type), buf(w, li, type), None if pre is None else buf(pre, li, type),
+                                               (empty_rows(rows, d_in, li, out_type), 0)])
+    within(values_of(out[3], rows, d_in, li, out_type), oo.linear_grad_input(dy, w, pre, act),
+           linear_grad_input_bound(dy, w, pre, act, out_type), "dx")
+    out = call(emu, tmp_path, 4, numbers, [], [buf(dy, lo, type), buf(x, li, type), (empty_rows(d_out, d_in, li, out_type), 0),
+                                               (np.full(d_out, np.nan, np.float32), 0) if bias else None])
+    want, bound = oo.linear_grad_weight(dy, x), linear_grad_weight_bounds(dy, x, out_type)
+    within(values_of(out[2], d_out, d_in, li, out_type), want[0], bound[0], "dw")
+    if bias:
+        within(out[3], want[1], bound[1], "dbias")
+
+
+@pytest.mark.parametrize("type", ["bf16", "f32"])
+def test_linear_weight_gradient_over_split_rows_and_no_rows(emu, tmp_path, type):
+    rng = np.random.default_rng(8)
+    rows, d_in, d_out = 1100, 24, 16
+    x, _, dy = matrices(rng, rows, d_in, d_out, type)
+    numbers = [KIND[type], fc.F32, 0, rows, d_in, d_out, d_in, d_in, d_out, d_out, d_out]
+    cfg = fc.make_linear_config(rows=rows, d_in=d_in, d_out=d_out, dtype=KIND[type], out_dtype=fc.F32)
+    assert fc.fastclip_linear_workspace_bytes(cfg, fc.LINEAR_BACKWARD_WEIGHT) > 0
+    room = [(np.full((d_out, d_in), np.nan, np.float32), 0), (np.full(d_out, np.nan, np.float32), 0)]
+    out = call(emu, tmp_path, 4, numbers, [], [(rows_of(dy, d_out, type), 0), (rows_of(x, d_in, type), 0), *room])
+    want, bound = oo.linear_grad_weight(dy, x), linear_grad_weight_bounds(dy, x, "f32")
+    within(out[2], want[0], bound[0], "dw")
+    within(out[3], want[1], bound[1], "dbias")
+    numbers[3] = 0
+    out = call(emu, tmp_path, 4, numbers, [], [None, None, *room])
+    assert np.all(out[2] == 0) and np.all(out[3] == 0)
+
+
+def test_linear_keeps_infinities_and_nan_to_their_rows(emu, tmp_path):
+    """The last stage of a depth of 72 takes 56 words per row from behind the matrix: none of them may reach a sum, and a row
+    of the tile that does not exist repeats one that does."""
+    rng = np.random.default_rng(9)
+    x, w, _ = matrices(rng, 5, 72, 16, "bf16")
+    x[2, 70] = np.inf
+    x[3, 1] = np.nan
+    numbers = [fc.BF16, fc.F32, 0, 5, 72, 16, 72, 72, 16, 16, 16]
+    out = call(emu, tmp_path, 2, numbers, [], [(rows_of(x, 72, "bf16"), 0), (rows_of(w, 72, "bf16"), 0), None, None,
+                                               (np.zeros((5, 16), np.float32), 0), None])
+    ok = [0, 1, 4]
+    within(out[4][ok], oo.linear(x[ok], w)[0], linear_bounds(x[ok], w, None, "", None, "f32", "bf16")[0], "y")
+    assert np.all(np.isnan(out[4][3])) and np.array_equal(out[4][2], np.where(w[:, 70] > 0, np.inf, -np.inf))
+
+
+ADAMW_SIZES = [1, 255, 256, 300, 4096, 4097, 5000, 0]
+
+
+@pytest.mark.parametrize("bits,grad,copy,skip", [(32, "f32", True, 0), (32, "bf16", False, 4), (8, "f32", True, 0),
+                                                 (8, "bf16", True, 2), (8, "bf16", False, 0)])
+def test_adamw_sources_on_the_host(emu, tmp_path, bits, grad, copy, skip):
+    """skip: bytes in front of the gradients (and, with 32-bit moments, of these), which puts a tensor on the single loads."""
+    rng = np.random.default_rng(bits + skip)
+    kw = dict(step=7, lr=1e-2, beta1=0.9, beta2=0.98, eps=1e-8)
+    seed = 12345
+    buffers, tensors, decays = [], [], []
+    for n in ADAMW_SIZES:
+        p = rng.normal(0, 0.1, n).astype(np.float32)
+        g = held((rng.normal(0, 1, n) * np.exp(rng.normal(0, 2, n)) * (rng.random(n) > 0.2)).astype(np.float32), grad)
+        blocks = -(-n // 256)
+        if bits == 32:
+            m, v = rng.normal(0, 0.3, n).astype(np.float32), (rng.random(n) * 0.5).astype(np.float32)
+            mv, vv, me, ve = m, v, None, None
+        else:
+            m, v = rng.integers(0, 256, n).astype(np.uint8), rng.integers(0, 256, n).astype(np.uint8)
+            m[(m & 127) > 120] = 0
+            v[v > 248] = 0
+            me, ve = rng.integers(100, 128, blocks).astype(np.uint8), rng.integers(100, 128, blocks).astype(np.uint8)
+            mv, vv = oo.decode(m, me, False), oo.decode(v, ve, True)
+        tensors.append((p, g, mv, vv))
+        decays.append(0.1 if n % 2 else 0.0)
+        gb = (g.view(np.uint32) >> 16).astype(np.uint16) if grad == "bf16" else g
+        buffers += [(p, 0), (gb, skip), (m, skip if bits == 32 else 1 if skip else 0), (v, 0),
+                    (np.zeros(n, np.uint16), 0) if copy else None, None if me is None else (me, 0), None if ve is None else (ve, 0)]
+    out = call(emu, tmp_path, 5, [bits, KIND[grad], seed, kw["step"], *ADAMW_SIZES],
+               [kw["lr"], kw["beta1"], kw["beta2"], kw["eps"], *decays], buffers)
+    for k, (n, (p, g, mv, vv)) in enumerate(zip(ADAMW_SIZES, tensors)):
+        if n == 0:
+            continue
+        got = out[7 * k:7 * k + 7]
+        want_p, want_m, want_v = oo.adamw(p, g, mv, vv, weight_decay=decays[k], **kw)
+        moved = np.abs(want_p - p)
+        within(got[0], want_p, 2 * U * np.abs(want_p) + 24 * U * moved + 4 * U * 1e-3 * np.abs(p) + 1e-37, "p")
+        if copy:
+            assert np.array_equal(got[4], (round_to_bf16(got[0]).view(np.uint32) >> 16).astype(np.uint16))
+        if bits == 32:
+            within(got[2], want_m, 3 * U * (0.9 * np.abs(mv) + 0.1 * np.abs(g)) + 1e-37, "m")
+            within(got[3], want_v, 5 * U * (0.98 * np.abs(vv) + 0.02 * g.astype(np.float64) ** 2) + 1e-37, "v")
+        else:
+            lo, hi = oo.random_halves(seed, k, n)
+            for which, x, r in ((2, want_m, lo), (3, want_v, hi)):
+                codes, exps = oo.encode(x, r, which == 3)
+                assert np.array_equal(got[which + 3], exps) and np.array_equal(got[which], codes), (n, which)
+                values = call(emu, tmp_path, 6, [which - 1, n], [], [(codes, 0), (exps, 0), (np.full(n, np.nan, np.float32), 0)])
+                assert np.array_equal(values[2].astype(np.float64), oo.decode(codes, exps, which == 3))
+
+
+def test_adamw_eight_bit_moments_of_extreme_size(emu, tmp_path):
+    """Blocks of zeros, of the smallest and of the largest magnitudes, and of moments that are not finite."""
+    n = 256 * 5
+    g = np.zeros(n, np.float32)
+    g[256:512] = 1e-42
+    g[512:768] = np.float32(3e38)
+    g[768] = np.inf
+    g[1024:1280] = 10.0 ** np.linspace(-30, 18, 256)
+    buffers = [(np.zeros(n, np.float32), 0), (g, 0), (np.zeros(n, np.uint8), 0), (np.zeros(n, np.uint8), 0), None,
+               (np.zeros(5, np.uint8), 0), (np.zeros(5, np.uint8), 0)]
+    out = call(emu, tmp_path, 5, [8, fc.F32, 1, 1, n], [1e-3, 0.9, 0.98, 1e-8, 0.0], buffers)
+    assert np.all(out[2][:256] == 0) and np.all(out[3][:256] == 0) and np.all(out[0][:256] == 0)
+    lo, hi = oo.random_halves(1, 0, n)
+    b1, b2 = float(np.float32(0.9)), float(np.float32(0.98))
+    for at in (256, 1024):
+        part = slice(at, at + 256)
+        x = g[part].astype(np.float64)
+        codes, exps = oo.encode((1 - b1) * x, lo[part], False)
+        assert np.array_equal(out[2][part], codes) and out[5][at // 256] == exps[0]
+        codes, exps = oo.encode((1 - b2) * x * x, hi[part], True)
+        assert np.array_equal(out[3][part], codes) and out[6][at // 256] == exps[0]
+    assert np.all(out[3][512:768] == 255) and out[6][2] == 126 + 127      # v beyond the range: the largest code
+    assert out[2][768] == 127 and out[3][768] == 255 and np.isnan(out[0][768])
