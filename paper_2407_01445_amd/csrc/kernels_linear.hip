@@ -29,9 +29,10 @@ __device__ __forceinline__ void dma16_from(const void* lane_address, uint32_t ld
 // rows which a read touches per cycle cover the banks.
 __device__ __forceinline__ int row_swizzle(int row) { return (row >> 1) & 7; }
 // LDS image of an operand by depth, T columns = T / 8 pieces a row of k: pieces moved by multiples of four, so that the 4 rows x
-// 64 bytes which a transposing read touches per cycle cover the banks.
+// 64 bytes which a transposing read touches per cycle cover the banks (rows an odd multiple of 128 bytes apart need it for
+// every second pair only).
 template <int T>
-__device__ __forceinline__ int depth_swizzle(int k) { return T == 64 ? ((k >> 1) & 1) << 2 : (k & 3) << 2; }
+__device__ __forceinline__ int depth_swizzle(int k) { return T % 128 ? ((k >> 1) & 1) << 2 : (k & 3) << 2; }
 
 // One operand of a tile: T rows (columns) of the output from `first` on, WAVES wavefronts fetching.
 template <int T, bool BY_DEPTH, int WAVES>
@@ -42,11 +43,10 @@ struct Operand {
   int64_t ld;
   int lane, wave;
   uint32_t off[kLoads];                          // byte offset of this lane's words of a stage
-  __device__ __forceinline__ int pieces() const { return T / 8; }
   // row of k (by depth) or chunk of k (by rows) inside a stage that this lane fetches with load i
   __device__ __forceinline__ int depth_of(int i) const {
     const int f = wave * kLoads + i;
-    if constexpr (BY_DEPTH) return f * (64 / (T / 8)) + lane / (T / 8);
+    if constexpr (BY_DEPTH) return (f * 64 + lane) / (T / 8);
     return 8 * ((lane & 7) ^ row_swizzle(8 * f + (lane >> 3)));
   }
   __device__ __forceinline__ void open(const bf16_t* matrix, int64_t ld_, int64_t first, int64_t count, int lane_, int wave_) {
@@ -57,7 +57,7 @@ struct Operand {
     for (int i = 0; i < kLoads; ++i) {
       const int f = wave * kLoads + i, d = depth_of(i);
       if constexpr (BY_DEPTH) {
-        int piece = (lane % (T / 8)) ^ depth_swizzle<T>(d);
+        int piece = ((f * 64 + lane) % (T / 8)) ^ depth_swizzle<T>(d);
         piece = piece * 8 < left ? piece : left / 8 - 1;
         off[i] = (uint32_t)d * (uint32_t)ld * 2u + (uint32_t)piece * 16u;
       } else {
@@ -112,18 +112,24 @@ __device__ __forceinline__ void exchange_halves(float (&v)[8]) {
   }
 }
 
-// WN x WM wavefronts, each with NI x NJ blocks of 32 x 32: 32 NI WN columns by 32 NJ WM rows of the output, S stages in flight.
+// A tile: WN x WM wavefronts, each with NI x NJ blocks of 32 x 32: 32 NI WN columns by 32 NJ WM rows of the output, S stages in
+// flight.
 template <bool PD, bool QD, int NI, int NJ, int WN, int WM, int S>
-__global__ void __launch_bounds__(64 * WN * WM) k_linear_bf16(LinearArgs a, uint32_t tiles_m, uint32_t tiles_n, int64_t slice) {
-  constexpr int TN = 32 * NI * WN, TM = 32 * NJ * WM, WAVES = WN * WM;
+struct Tile {
+  static constexpr int TN = 32 * NI * WN, TM = 32 * NJ * WM, WAVES = WN * WM;
   typedef Operand<TM, PD, WAVES> OpP;
   typedef Operand<TN, QD, WAVES> OpQ;
-  constexpr int kStage = OpP::kBytes + OpQ::kBytes, kRequests = OpP::kLoads + OpQ::kLoads;
-  __shared__ __attribute__((aligned(1024))) char ring[S * kStage];
+  static constexpr int kStage = OpP::kBytes + OpQ::kBytes, kRequests = OpP::kLoads + OpQ::kLoads, kRing = S * kStage;
+  // first row m0, column number `col` of `cols`, split number `split` of `splits`
+  static __device__ __forceinline__ void run(const LinearArgs& a, char* ring, int64_t m0, int64_t col, int64_t cols, int split,
+                                             int splits, int64_t slice);
+};
+template <bool PD, bool QD, int NI, int NJ, int WN, int WM, int S>
+__device__ __forceinline__ void Tile<PD, QD, NI, NJ, WN, WM, S>::run(const LinearArgs& a, char* ring, int64_t m0, int64_t col,
+                                                                     int64_t cols, int split, int splits, int64_t slice) {
   const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   const int wn = wave % WN, wm = wave / WN, lr = lane & 31, hk = lane >> 5;
-  const TilePlace place = tile_place(blockIdx.x, gridDim.x, tiles_m, tiles_n);
-  const int64_t m0 = place.m * TM, n0 = place.n * TN, k0 = place.split * slice;
+  const int64_t n0 = col * TN, k0 = split * slice;
   const int64_t end = k0 + slice < a.K ? k0 + slice : a.K;
   const int stages = (int)((end - k0 + kDepth - 1) / kDepth);
   OpP p;
@@ -131,8 +137,8 @@ __global__ void __launch_bounds__(64 * WN * WM) k_linear_bf16(LinearArgs a, uint
   p.open((const bf16_t*)a.p, a.ldp, m0, a.M, lane, wave);
   q.open((const bf16_t*)a.q, a.ldq, n0, a.N, lane, wave);
   const uint32_t ring_at = lds_addr(ring);
-  auto request = [&](int stage) {
-    const uint32_t slot = ring_at + (uint32_t)(stage % S) * (uint32_t)kStage;
+  auto request = [&](int stage, int at) {
+    const uint32_t slot = ring_at + (uint32_t)at * (uint32_t)kStage;
     p.request(k0 + (int64_t)stage * kDepth, end, slot);
     q.request(k0 + (int64_t)stage * kDepth, end, slot + (uint32_t)OpP::kBytes);
   };
@@ -143,14 +149,18 @@ __global__ void __launch_bounds__(64 * WN * WM) k_linear_bf16(LinearArgs a, uint
     for (int j = 0; j < NJ; ++j)
 #pragma unroll
       for (int v = 0; v < 16; ++v) acc[i][j][v] = 0.f;
-  const bool sums = PD && QD && a.dbias && place.n == 0 && wn == 0;      // this wavefront also sums P over the depth
+  // The sum of P over the depth: with splits every column of tiles and of wavefronts has its share of the stages (`sharing` in
+  // all) and leaves a partial sum; without, where there is nobody to add them up, those of the first column have them all.
+  const bool bias_sums = PD && QD && a.dbias;
+  const int sharing = splits > 1 ? (int)cols * WN : 1, share = splits > 1 ? (int)col * WN + wn : (col == 0 && wn == 0 ? 0 : 1);
   float total[NJ];
 #pragma unroll
   for (int j = 0; j < NJ; ++j) total[j] = 0.f;
 
 #pragma unroll
   for (int s = 0; s < S - 1; ++s)
-    if (s < stages) request(s);
+    if (s < stages) request(s, s);
+  int here = 0, before = S - 1;               // places of stages g and g - 1 (and g + S - 1)
   for (int g = 0; g < stages; ++g) {
     // stage g has landed, and every wavefront is done with stage g - 1, whose place the next request takes
     if (g + S - 2 < stages) wait_vmcnt<(S - 2) * kRequests>();
@@ -158,9 +168,12 @@ __global__ void __launch_bounds__(64 * WN * WM) k_linear_bf16(LinearArgs a, uint
     FC_FENCE();
     __builtin_amdgcn_s_barrier();
     FC_FENCE();
-    if (g + S - 1 < stages) request(g + S - 1);
-    const char* panel_p = ring + (g % S) * kStage;
+    if (g + S - 1 < stages) request(g + S - 1, before);
+    const char* panel_p = ring + here * kStage;
+    before = here;
+    here = here + 1 < S ? here + 1 : 0;
     const char* panel_q = panel_p + OpP::kBytes;
+    const bool sums = bias_sums && g % sharing == share;
     float some[NJ];
 #pragma unroll
     for (int j = 0; j < NJ; ++j) some[j] = 0.f;
@@ -196,39 +209,64 @@ __global__ void __launch_bounds__(64 * WN * WM) k_linear_bf16(LinearArgs a, uint
     }
   }
 
-  const bool split = gridDim.x > tiles_m * tiles_n;
-  if (sums) {
+  if (bias_sums && share < sharing) {
 #pragma unroll
     for (int j = 0; j < NJ; ++j) {
       const float s = total[j] + __shfl_xor(total[j], 32);
       const int64_t m = m0 + (wm * NJ + j) * 32 + lr;
-      float* to = split ? a.partial + (int64_t)(gridDim.x / (tiles_m * tiles_n)) * a.M * a.N + place.split * a.M : a.dbias;
+      float* to = splits > 1 ? a.partial + (int64_t)splits * a.M * a.N + ((int64_t)split * sharing + share) * a.M : a.dbias;
       if (hk == 0 && m < a.M) to[m] = s;
     }
   }
+  auto values = [&](int j, int h, float (&v)[8]) {
 #pragma unroll
-  for (int j = 0; j < NJ; ++j) {
-    const int64_t m = m0 + (wm * NJ + j) * 32 + lr;
+    for (int e = 0; e < 8; ++e) v[e] = acc[h >> 1][j][8 * (h & 1) + e];
+    exchange_halves(v);
+  };
+  auto m_of = [&](int j) { return m0 + (wm * NJ + j) * 32 + lr; };
+  auto n_of = [&](int h) { return n0 + wn * NI * 32 + 16 * h + 8 * hk; };
+  if (splits > 1) {
 #pragma unroll
-    for (int i = 0; i < NI; ++i)
+    for (int j = 0; j < NJ; ++j)
 #pragma unroll
-      for (int h = 0; h < 2; ++h) {
+      for (int h = 0; h < 2 * NI; ++h) {
         float v[8];
-#pragma unroll
-        for (int e = 0; e < 8; ++e) v[e] = acc[i][j][8 * h + e];
-        exchange_halves(v);
-        const int64_t n = n0 + (wn * NI + i) * 32 + 16 * h + 8 * hk;
-        if (m < a.M && n < a.N) {
-          if (split) store_f32<8>(a.partial + ((int64_t)place.split * a.M + m) * a.N + n, v);
-          else finish_values<true, 8>(a, v, m, n);
-        }
+        values(j, h, v);
+        if (m_of(j) < a.M && n_of(h) < a.N) store_f32<8>(a.partial + ((int64_t)split * a.M + m_of(j)) * a.N + n_of(h), v);
       }
+  } else {
+    finish_tile<!PD, NJ, 2 * NI>(a, values, m_of, n_of);
+  }
+}
+
+template <bool PD, bool QD, int NI, int NJ, int WN, int WM, int S>
+__global__ void __launch_bounds__(64 * WN * WM) k_linear_bf16(LinearArgs a, uint32_t rows, uint32_t cols, int splits, int64_t slice) {
+  typedef Tile<PD, QD, NI, NJ, WN, WM, S> T;
+  __shared__ __attribute__((aligned(1024))) char ring[T::kRing];
+  const TilePlace place = tile_place(blockIdx.x, gridDim.x, rows, cols);
+  T::run(a, ring, place.m * T::TM, place.n, cols, place.split, splits, slice);
+}
+
+// Bands of 192 rows, then bands of 128, by 128 columns, two workgroups to a compute unit.
+template <bool PD, bool QD>
+__global__ void __launch_bounds__(256, 2) k_linear_bands(LinearArgs a, uint32_t high, uint32_t low, uint32_t cols, int splits,
+                                                         int64_t slice) {
+  typedef Tile<PD, QD, 2, 3, 2, 2, 2> High;
+  typedef Tile<PD, QD, 2, 2, 2, 2, 2> Low;
+  __shared__ __attribute__((aligned(1024))) char ring[High::kRing];
+  const uint32_t first = high * cols * (uint32_t)splits;
+  if (blockIdx.x < first) {
+    const TilePlace place = tile_place(blockIdx.x, first, high, cols);
+    High::run(a, ring, place.m * High::TM, place.n, cols, place.split, splits, slice);
+  } else {
+    const TilePlace place = tile_place(blockIdx.x - first, gridDim.x - first, low, cols);
+    Low::run(a, ring, (int64_t)high * High::TM + place.m * Low::TM, place.n, cols, place.split, splits, slice);
   }
 }
 
 // ---- sums of splits -----------------------------------------------------------------------------------------------------
 template <bool BF16, int V>
-__global__ void __launch_bounds__(256) k_linear_join(LinearArgs a, int splits) {
+__global__ void __launch_bounds__(256) k_linear_join(LinearArgs a, int splits, int bias_parts) {
   const int64_t per_row = a.N / V, total = a.M * per_row;
   const int64_t t = (int64_t)blockIdx.x * 256 + threadIdx.x;
   if (t < total) {
@@ -249,7 +287,7 @@ __global__ void __launch_bounds__(256) k_linear_join(LinearArgs a, int splits) {
     const float* part = a.partial + (int64_t)splits * a.M * a.N + m;
     float z = 0.f;
 #pragma unroll 4
-    for (int s = 0; s < splits; ++s) z += part[(int64_t)s * a.M];
+    for (int s = 0; s < bias_parts; ++s) z += part[(int64_t)s * a.M];
     a.dbias[m] = z;
   }
 }
@@ -258,8 +296,8 @@ void launch_linear_join(const LinearArgs& a, const LinearPlan& plan, hipStream_t
   const int v = a.bf16 ? 8 : 1;
   const int64_t threads = a.M * (a.N / v) + (a.dbias ? a.M : 0);
   const dim3 grid((unsigned)((threads + 255) / 256));
-  if (a.bf16) hipLaunchKernelGGL((k_linear_join<true, 8>), grid, dim3(256), 0, s, a, plan.splits);
-  else hipLaunchKernelGGL((k_linear_join<false, 1>), grid, dim3(256), 0, s, a, plan.splits);
+  if (a.bf16) hipLaunchKernelGGL((k_linear_join<true, 8>), grid, dim3(256), 0, s, a, plan.splits, plan.bias_parts);
+  else hipLaunchKernelGGL((k_linear_join<false, 1>), grid, dim3(256), 0, s, a, plan.splits, plan.bias_parts);
 }
 
 // The gradient of the weight of no rows.
@@ -276,32 +314,82 @@ void launch_linear_empty(const LinearArgs& a, hipStream_t s) {
 }
 
 // ---- plan -----------------------------------------------------------------------------------------------------------------
+// Measured (one MI355X, us; a stage is 64 of k).  A stage of a 64 x 64 tile takes 0.33 where its workgroup has a compute unit to
+// itself, 0.46 and 0.6 where two and three share it; of 128 x 128 0.62 and, two on a compute unit, 0.96; of 192 x 128 1.19, two
+// on a compute unit; of 256 x 256, alone, 1.5.  A round of workgroups starts and ends in 2, 3, 4.5 and 20 (epilogue and
+// stores of two workgroups on a compute unit pass beneath the other one's products; the large tile has nobody).  Splits: a
+// launch and the traffic of their partial sums.
+static double rounds_of(int64_t n, double deep, int per_cu, const double (&stage)[3], double ends) {
+  const int64_t places = 256 * per_cu, full = n / places, rest = n % places;
+  double t = (double)full * (deep * stage[per_cu - 1] + ends);
+  if (rest) t += deep * stage[rest <= 256 ? 0 : (rest <= 512 ? 1 : 2)] + ends;
+  return t;
+}
+static const double kStage64[3] = {0.33, 0.46, 0.60}, kStage128[3] = {0.62, 0.96, 0.96}, kStage192[3] = {0.80, 1.19, 1.19},
+                    kStage256[3] = {1.50, 1.50, 1.50}, kStageF32[3] = {2.0, 2.5, 3.0};
+
+// What takes the least time by the figures above.  16384 rows of 1024 -> 4096 with GELU and pre kept: 256 x 256 221, bands of 192
+// rows 190, with the last 1024 rows in bands of 128 (which fill the last round) 182; 4096 -> 4096: 256 x 256 456, bands 481.
+// 1024 rows of 1024 -> 1024: 64 x 64 9.5, 128 x 128 13.5; 4096 rows: 19 and 15.  128 rows of 4096 -> 512: one split 25, eight 10.
 LinearPlan plan_linear(int64_t M, int64_t N, int64_t K, bool bf16, bool, bool, bool dbias) {
-  LinearPlan best = {64, 1, K, 0};
-  auto tiles = [&](int64_t t) { return ((M + t - 1) / t) * ((N + t - 1) / t); };
-  if (bf16) best.tile = tiles(256) >= 192 ? 256 : (tiles(128) >= 192 ? 128 : 64);
-  const int64_t stages = (K + kDepth - 1) / kDepth, n = tiles(best.tile);
-  int64_t splits = best.tile < 256 && n < 256 ? 512 / n : 1;
-  if (splits > stages / 4) splits = stages / 4;
-  while (splits > 1 && splits * M * N > ((int64_t)16 << 20)) --splits;
-  if (splits < 1) splits = 1;
-  const int64_t slice = (stages + splits - 1) / splits;
-  best.splits = (int)((stages + slice - 1) / slice);
-  best.slice = slice * kDepth;
-  if (best.splits > 1) best.bytes = round_up(sizeof(float) * (size_t)best.splits * (size_t)(M * N + (dbias ? M : 0)), 256);
+  static const int kSplits[] = {1, 2, 3, 4, 6, 8, 12, 16, 24, 32, 48, 64};
+  auto count = [](int64_t x, int64_t t) { return (x + t - 1) / t; };
+  const int64_t stages = count(K, kDepth), n64 = count(M, 64) * count(N, 64), cols = count(N, 128), n128 = count(M, 128) * cols,
+                n256 = count(M, 256) * count(N, 256);
+  LinearPlan best = {0, 0, 0, 1, 0, 1, 0};
+  double best_cost = 0.0;
+  for (int s : kSplits) {
+    const int64_t slice = count(stages, s);
+    if (s > 1 && (s > stages || s * M * N > ((int64_t)32 << 20) || n64 * s > 4096)) break;
+    if (count(stages, slice) != s) continue;                                // every split gets at least one stage
+    const double deep = (double)slice, join = s > 1 ? 2.6 + (double)(2 * s + 1) * (double)(M * N) * 4.0 / 5.5e6 : 0.0;
+    auto consider = [&](int tile, int64_t high, int64_t low, double cost) {
+      cost += join;
+      if (best.tile && cost >= best_cost) return;
+      best_cost = cost;
+      best.tile = tile; best.high = (int)high; best.low = (int)low; best.splits = s; best.slice = slice * kDepth;
+    };
+    if (n64 <= 4096 || !bf16) consider(64, 0, 0, rounds_of(n64 * s, deep, 3, bf16 ? kStage64 : kStageF32, 2.0));
+    if (!bf16 || n64 <= 256) continue;
+    consider(128, 0, count(M, 128), rounds_of(n128 * s, deep, 2, kStage128, 3.0));
+    if (n256 * s >= 128) consider(256, 0, 0, rounds_of(n256 * s, deep, 1, kStage256, 20.0));
+    if (s > 1 || n128 <= 512) continue;
+    // whole rounds of 192-row bands, or what leaves up to 24 bands of 128 rows for the last one
+    for (int64_t low = 0; low <= 24 && low * 128 < M; ++low) {
+      const int64_t high = count(M - low * 128, 192);
+      if (low > 0 && high * 192 + (low - 1) * 128 >= M) continue;           // every band has rows
+      const int64_t rest = high * cols % 512;
+      double cost = rounds_of(high * cols - rest, deep, 2, kStage192, 4.5);
+      // the last of them and the others side by side: two thirds of a place for each of the latter
+      const int64_t mixed = rest + (2 * low * cols + 2) / 3;
+      cost += rounds_of(mixed, deep, 2, kStage192, 4.5);
+      consider(128, high, low, cost);
+    }
+  }
+  best.bias_parts = best.tile == 128 ? 2 * (int)cols : (best.tile == 256 ? 4 * (int)count(N, 256) : 2 * (int)count(N, 64));
+  if (!bf16) best.bias_parts = 1;
+  best.bias_parts *= best.splits;
+  if (best.splits > 1)
+    best.bytes = round_up(sizeof(float) * ((size_t)best.splits * (size_t)(M * N) + (dbias ? (size_t)best.bias_parts * (size_t)M : 0)), 256);
   return best;
 }
 
 template <bool PD, bool QD>
 static void launch_form(const LinearArgs& a, const LinearPlan& plan, hipStream_t s) {
-  const uint32_t tm = (uint32_t)((a.M + plan.tile - 1) / plan.tile), tn = (uint32_t)((a.N + plan.tile - 1) / plan.tile);
-  const dim3 grid(tm * tn * (uint32_t)plan.splits);
+  const uint32_t splits = (uint32_t)plan.splits;
+  if (plan.tile == 128) {
+    const uint32_t high = (uint32_t)plan.high, low = (uint32_t)plan.low, cols = (uint32_t)((a.N + 127) / 128);
+    hipLaunchKernelGGL((k_linear_bands<PD, QD>), dim3((high + low) * cols * splits), dim3(256), 0, s, a, high, low, cols,
+                       plan.splits, plan.slice);
+    return;
+  }
+  const uint32_t rows = (uint32_t)((a.M + plan.tile - 1) / plan.tile), cols = (uint32_t)((a.N + plan.tile - 1) / plan.tile);
   if (plan.tile == 256)
-    hipLaunchKernelGGL((k_linear_bf16<PD, QD, 2, 4, 4, 2, 2>), grid, dim3(512), 0, s, a, tm, tn, plan.slice);
-  else if (plan.tile == 128)
-    hipLaunchKernelGGL((k_linear_bf16<PD, QD, 2, 2, 2, 2, 2>), grid, dim3(256), 0, s, a, tm, tn, plan.slice);
+    hipLaunchKernelGGL((k_linear_bf16<PD, QD, 2, 4, 4, 2, 2>), dim3(rows * cols * splits), dim3(512), 0, s, a, rows, cols,
+                       plan.splits, plan.slice);
   else
-    hipLaunchKernelGGL((k_linear_bf16<PD, QD, 1, 1, 2, 2, 3>), grid, dim3(256), 0, s, a, tm, tn, plan.slice);
+    hipLaunchKernelGGL((k_linear_bf16<PD, QD, 1, 1, 2, 2, 3>), dim3(rows * cols * splits), dim3(256), 0, s, a, rows, cols,
+                       plan.splits, plan.slice);
 }
 
 void launch_linear_bf16(const LinearArgs& a, const LinearPlan& plan, hipStream_t s) {

@@ -136,6 +136,89 @@ __device__ __forceinline__ void finish_values(const LinearArgs& a, float (&z)[V]
   else finish_values_act<BF16, FASTCLIP_ACT_NONE, V>(a, z, m, n);
 }
 
+// ---- the epilogue of a wavefront's part of a tile --------------------------------------------------------------------------
+//
+// Eight neighbouring values of an output row at a time, groups h = 0 .. G - 1 side by side in a row of blocks.  Vector memory
+// operations complete in the order of their issue, stores too: a load behind stores waits for them.  So everything that the
+// epilogue reads is requested ahead of the stores: the bias before the first, residual and pre three groups
+// ahead.
+struct Held8 { u32x4 lo, hi; };                 // eight bf16 (lo) or fp32 values as they lie in memory
+__device__ __forceinline__ void hold(Held8& x, const void* p, int64_t at, bool bf16) {
+  if (bf16) {
+    x.lo = *(const u32x4*)((const bf16_t*)p + at);
+  } else {
+    x.lo = *(const u32x4*)((const float*)p + at);
+    x.hi = *(const u32x4*)((const float*)p + at + 4);
+  }
+}
+__device__ __forceinline__ float held_value(const Held8& x, int i, bool bf16) {
+  const float wide = __uint_as_float(i < 4 ? x.lo[i & 3] : x.hi[i & 3]);
+  const uint32_t w = x.lo[i >> 1];
+  return bf16 ? __uint_as_float(i & 1 ? w & 0xffff0000u : w << 16) : wide;
+}
+// values(j, h, v): the eight sums of group h of row of blocks j, this lane's; its output row is m_of(j), its first column n_of(h).
+template <int ACT, int ROWS, int G, typename Values, typename MOf, typename NOf>
+__device__ __forceinline__ void finish_tile_act(const LinearArgs& a, Values&& values, MOf&& m_of, NOf&& n_of) {
+  const bool slope = ACT != FASTCLIP_ACT_NONE && a.pre_in, out_bf16 = a.out_bf16;
+  float bias[G][8];
+#pragma unroll
+  for (int h = 0; h < G; ++h) {
+#pragma unroll
+    for (int e = 0; e < 8; ++e) bias[h][e] = 0.f;
+    if (a.bias) load_f32<8>(bias[h], a.bias + (n_of(h) < a.N ? n_of(h) : a.N - 8));
+  }
+  constexpr int kAhead = 3;                      // groups
+  Held8 extra[kAhead + 1];                       // pre_in or residual: a call has at most one of the two
+  auto request = [&](int t) {
+    const int64_t m = m_of(t / G) < a.M ? m_of(t / G) : a.M - 1, n = n_of(t % G) < a.N ? n_of(t % G) : a.N - 8;
+    if (slope) hold(extra[t % (kAhead + 1)], a.pre_in, m * a.ld_pre + n, true);
+    else if (a.residual) hold(extra[t % (kAhead + 1)], a.residual, m * a.ld_res + n, out_bf16);
+  };
+#pragma unroll
+  for (int t = 0; t < kAhead && t < ROWS * G; ++t) request(t);
+#pragma unroll
+  for (int j = 0; j < ROWS; ++j) {
+    const int64_t m = m_of(j);
+    char* out = (char*)a.out + (m * a.ld_out) * (out_bf16 ? 2 : 4);
+    bf16_t* pre = (bf16_t*)a.pre_out + m * a.ld_pre;
+#pragma unroll
+    for (int h = 0; h < G; ++h) {
+      const int t = j * G + h;
+      if (t + kAhead < ROWS * G) request(t + kAhead);
+      const Held8& with = extra[t % (kAhead + 1)];
+      const int64_t n = n_of(h);
+      float v[8];
+      values(j, h, v);
+#pragma unroll
+      for (int e = 0; e < 8; ++e) v[e] += bias[h][e];
+      const bool in = m < a.M && n < a.N;
+      if (a.pre_out && in) store_bf16<8>(pre + n, v);
+      if (slope) {
+#pragma unroll
+        for (int e = 0; e < 8; ++e) v[e] *= activation_slope<ACT>(held_value(with, e, true));
+      } else if constexpr (ACT != FASTCLIP_ACT_NONE) {
+#pragma unroll
+        for (int e = 0; e < 8; ++e) v[e] = activate<ACT>(v[e]);
+      }
+      if (a.residual) {
+#pragma unroll
+        for (int e = 0; e < 8; ++e) v[e] += held_value(with, e, out_bf16);
+      }
+      if (in) {
+        if (out_bf16) store_bf16<8>((bf16_t*)out + n, v);
+        else store_f32<8>((float*)out + n, v);
+      }
+      FC_PIN();      // the sums of one group at a time in registers of their own
+    }
+  }
+}
+template <bool HAS_ACT, int ROWS, int G, typename Values, typename MOf, typename NOf>
+__device__ __forceinline__ void finish_tile(const LinearArgs& a, Values&& values, MOf&& m_of, NOf&& n_of) {
+  if (HAS_ACT && a.act == FASTCLIP_ACT_GELU) finish_tile_act<FASTCLIP_ACT_GELU, ROWS, G>(a, values, m_of, n_of);
+  else if (HAS_ACT && a.act == FASTCLIP_ACT_QUICK_GELU) finish_tile_act<FASTCLIP_ACT_QUICK_GELU, ROWS, G>(a, values, m_of, n_of);
+  else finish_tile_act<FASTCLIP_ACT_NONE, ROWS, G>(a, values, m_of, n_of);
+}
+
 // Which output tile and split a workgroup takes.  Workgroups go to the eight XCDs in turn, each with an L2 of its own: those of
 // one XCD take neighbouring tiles, eight rows of tiles by as many columns as there are.
 struct TilePlace { int64_t m, n; int split; };

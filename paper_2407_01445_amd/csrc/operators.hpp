@@ -42,12 +42,14 @@ struct LinearArgs {
   int64_t ld_pre;
   int act;                 // fastclip_activation: of z, or of which the derivative is taken with pre_in
   float* dbias;            // gradient of the weight: [M], sums of P over k, or nullptr
-  float* partial;          // workspace: [splits][M][N] and behind them [splits][M] for dbias
+  float* partial;          // workspace: [splits][M][N] and behind them [bias_parts][M] for dbias
 };
 struct LinearPlan {
-  int tile;                // rows and columns of a workgroup's output tile
+  int tile;                // 64, 256: rows and columns of a workgroup's output tile; 128: bands of
+  int high, low;           // ... 192 and then of 128 rows, 128 columns
   int splits;              // workgroups over the depth of a tile
   int64_t slice;           // depth of a split
+  int bias_parts;          // partial sums of dbias, with splits
   size_t bytes;            // workspace
 };
 LinearPlan plan_linear(int64_t M, int64_t N, int64_t K, bool bf16, bool p_by_depth, bool q_by_depth, bool dbias);

@@ -7,6 +7,7 @@
 #define main emu_step_main
 #include "emu_main.cpp"
 #undef main
+#include "operators.hpp"
 
 static void* aligned_room(size_t bytes) {
   void* p = nullptr;
@@ -68,6 +69,31 @@ int main(int argc, char** argv) {
     if (st == FASTCLIP_OK) st = fastclip_adamw_step(&c, &table, nullptr);
   } else if (op == 6) {
     st = fastclip_adamw_state_values((int32_t)n[0], (uint8_t*)b[0], (uint8_t*)b[1], n[1], (float*)b[2], nullptr);
+  }
+  if (op == 7) {                   // plans of products M x N over K: every workgroup has rows, columns and depth, and nothing is left out
+    st = FASTCLIP_OK;
+    uint64_t x = 88172645463325252ull;
+    auto next = [&](int64_t hi, int64_t step) {          // spread over the logarithm
+      x ^= x << 13; x ^= x >> 7; x ^= x << 17;
+      const double r = (double)(x >> 11) / 9007199254740992.0;
+      const int64_t v = (int64_t)(pow((double)(hi + 1), r));
+      return (v + step - 1) / step * step;
+    };
+    for (int64_t i = 0; i < n[0] && st == FASTCLIP_OK; ++i) {
+      const bool bf16 = i % 4 != 0;
+      const int64_t M = next(40000, 1), N = next(9000, bf16 ? 8 : 1), K = next(20000, 1);
+      const fc::LinearPlan p = fc::plan_linear(M, N, K, bf16, false, false, true);
+      const bool tiles = p.tile == 64 || (bf16 && p.tile == 256) ||
+                         (bf16 && p.tile == 128 && p.high >= 0 && p.low >= 0 && p.high * 192 + p.low * 128 >= M &&
+                          (p.low ? p.high * 192 + (p.low - 1) * 128 < M : (p.high - 1) * 192 < M));
+      const bool depth = p.splits >= 1 && p.slice % 64 == 0 && p.splits * p.slice >= K && (p.splits - 1) * p.slice < K;
+      const size_t need = p.splits > 1 ? 4 * (size_t)(p.splits * M * N + p.bias_parts * M) : 0;
+      if (!tiles || !depth || p.bytes < need) {
+        fprintf(stderr, "plan of %ld x %ld over %ld: tile %d high %d low %d splits %d slice %ld\n", (long)M, (long)N, (long)K, p.tile,
+                p.high, p.low, p.splits, (long)p.slice);
+        st = FASTCLIP_ERR_SHAPE;
+      }
+    }
   }
   f = fopen(argv[2], "wb");
   if (!f) return 2;

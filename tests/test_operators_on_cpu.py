@@ -442,6 +442,11 @@ def test_linear_keeps_infinities_and_nan_to_their_rows(emu, tmp_path):
     assert np.all(np.isnan(out[4][3])) and np.array_equal(out[4][2], np.where(w[:, 70] > 0, np.inf, -np.inf))
 
 
+def test_linear_plans_leave_nothing_out(emu, tmp_path):
+    """20000 products of all sizes: every band of tiles has rows, every split depth, and together they cover the product."""
+    call(emu, tmp_path, 7, [20000], [], [])
+
+
 ADAMW_SIZES = [1, 255, 256, 300, 4096, 4097, 5000, 0]
 
 
