@@ -247,15 +247,16 @@ __global__ void __launch_bounds__(64 * WN * WM) k_linear_bf16(LinearArgs a, uint
   T::run(a, ring, place.m * T::TM, place.n, cols, place.split, splits, slice);
 }
 
-// Bands of 192 rows, then bands of 128, by 128 columns, two workgroups to a compute unit.
+// Bands of 192 rows, then bands of 128, by 128 columns, two workgroups to a compute unit.  No bands of 192 with P by depth: they
+// are no faster there (16384 rows, dw of 1024 x 4096: 173 us, 128 x 128 153, 256 x 256 142).
 template <bool PD, bool QD>
 __global__ void __launch_bounds__(256, 2) k_linear_bands(LinearArgs a, uint32_t high, uint32_t low, uint32_t cols, int splits,
                                                          int64_t slice) {
-  typedef Tile<PD, QD, 2, 3, 2, 2, 2> High;
+  typedef Tile<PD, QD, 2, PD ? 2 : 3, 2, 2, 2> High;
   typedef Tile<PD, QD, 2, 2, 2, 2, 2> Low;
   __shared__ __attribute__((aligned(1024))) char ring[High::kRing];
   const uint32_t first = high * cols * (uint32_t)splits;
-  if (blockIdx.x < first) {
+  if (!PD && blockIdx.x < first) {
     const TilePlace place = tile_place(blockIdx.x, first, high, cols);
     High::run(a, ring, place.m * High::TM, place.n, cols, place.split, splits, slice);
   } else {
@@ -265,39 +266,64 @@ __global__ void __launch_bounds__(256, 2) k_linear_bands(LinearArgs a, uint32_t 
 }
 
 // ---- sums of splits -----------------------------------------------------------------------------------------------------
-template <bool BF16, int V>
-__global__ void __launch_bounds__(256) k_linear_join(LinearArgs a, int splits, int bias_parts) {
-  const int64_t per_row = a.N / V, total = a.M * per_row;
-  const int64_t t = (int64_t)blockIdx.x * 256 + threadIdx.x;
-  if (t < total) {
-    const int64_t m = t / per_row, n = (t - m * per_row) * V;
+// V neighbouring values of the output by G lanes, each with every G-th split; behind the workgroups of the output those of dbias,
+// 32 values by 8 threads.  With one lane a value the loads of 64 splits follow each other: 24 us for 128 x 128 values, of which
+// the splits' products were 6.
+template <bool BF16, int V, int G>
+__global__ void __launch_bounds__(256) k_linear_join(LinearArgs a, int splits, int bias_parts, uint32_t out_groups) {
+  if (blockIdx.x < out_groups) {
+    const int64_t per_row = a.N / V, t = (int64_t)blockIdx.x * (256 / G) + threadIdx.x / G;
+    const bool in = t < a.M * per_row;
+    const int64_t m = in ? t / per_row : 0, n = in ? (t - m * per_row) * V : 0;
     float z[V];
 #pragma unroll
     for (int i = 0; i < V; ++i) z[i] = 0.f;
 #pragma unroll 4
-    for (int s = 0; s < splits; ++s) {
+    for (int s = threadIdx.x % G; s < splits; s += G) {
       float x[V];
       load_f32<V>(x, a.partial + ((int64_t)s * a.M + m) * a.N + n);
 #pragma unroll
       for (int i = 0; i < V; ++i) z[i] += x[i];
     }
-    finish_values<BF16, V>(a, z, m, n);
-  } else if (a.dbias && t - total < a.M) {
-    const int64_t m = t - total;
-    const float* part = a.partial + (int64_t)splits * a.M * a.N + m;
+#pragma unroll
+    for (int k = 1; k < G; k *= 2)
+#pragma unroll
+      for (int i = 0; i < V; ++i) z[i] += __shfl_xor(z[i], k);
+    if (in && threadIdx.x % G == 0) finish_values<BF16, V>(a, z, m, n);
+  } else {
+    __shared__ float sums[8][32];
+    const int at = threadIdx.x & 31, part = threadIdx.x >> 5;
+    const int64_t m = (int64_t)(blockIdx.x - out_groups) * 32 + at;
+    const float* from = a.partial + (int64_t)splits * a.M * a.N + (m < a.M ? m : 0);
     float z = 0.f;
-#pragma unroll 4
-    for (int s = 0; s < bias_parts; ++s) z += part[(int64_t)s * a.M];
-    a.dbias[m] = z;
+#pragma unroll 8
+    for (int s = part; s < bias_parts; s += 8) z += from[(int64_t)s * a.M];
+    sums[part][at] = z;
+    __syncthreads();
+    if (part == 0 && m < a.M) {
+      z = 0.f;
+#pragma unroll
+      for (int k = 0; k < 8; ++k) z += sums[k][at];
+      a.dbias[m] = z;
+    }
   }
 }
 
+template <bool BF16, int V, int G>
+static void launch_join(const LinearArgs& a, const LinearPlan& plan, hipStream_t s) {
+  const uint32_t out_groups = (uint32_t)((a.M * (a.N / V) * G + 255) / 256), bias_groups = a.dbias ? (uint32_t)((a.M + 31) / 32) : 0;
+  hipLaunchKernelGGL((k_linear_join<BF16, V, G>), dim3(out_groups + bias_groups), dim3(256), 0, s, a, plan.splits, plan.bias_parts,
+                     out_groups);
+}
 void launch_linear_join(const LinearArgs& a, const LinearPlan& plan, hipStream_t s) {
-  const int v = a.bf16 ? 8 : 1;
-  const int64_t threads = a.M * (a.N / v) + (a.dbias ? a.M : 0);
-  const dim3 grid((unsigned)((threads + 255) / 256));
-  if (a.bf16) hipLaunchKernelGGL((k_linear_join<true, 8>), grid, dim3(256), 0, s, a, plan.splits, plan.bias_parts);
-  else hipLaunchKernelGGL((k_linear_join<false, 1>), grid, dim3(256), 0, s, a, plan.splits, plan.bias_parts);
+  if (a.bf16) {
+    if (plan.splits < 4) launch_join<true, 8, 1>(a, plan, s);
+    else if (plan.splits < 16) launch_join<true, 8, 4>(a, plan, s);
+    else launch_join<true, 8, 16>(a, plan, s);
+  } else {
+    if (plan.splits < 4) launch_join<false, 1, 1>(a, plan, s);
+    else launch_join<false, 1, 4>(a, plan, s);
+  }
 }
 
 // The gradient of the weight of no rows.
@@ -315,23 +341,24 @@ void launch_linear_empty(const LinearArgs& a, hipStream_t s) {
 
 // ---- plan -----------------------------------------------------------------------------------------------------------------
 // Measured (one MI355X, us; a stage is 64 of k).  A stage of a 64 x 64 tile takes 0.33 where its workgroup has a compute unit to
-// itself, 0.46 and 0.6 where two and three share it; of 128 x 128 0.62 and, two on a compute unit, 0.96; of 192 x 128 1.19, two
-// on a compute unit; of 256 x 256, alone, 1.5.  A round of workgroups starts and ends in 2, 3, 4.5 and 20 (epilogue and
-// stores of two workgroups on a compute unit pass beneath the other one's products; the large tile has nobody).  Splits: a
-// launch and the traffic of their partial sums.
+// itself, 0.46 and 0.6 where two and three share it; of 128 x 128 0.62 and, two on a compute unit, 0.96; of 192 x 128 0.8 and 1.23;
+// of 256 x 256, alone, 1.67; the small tiles a sixth more with both operands by depth.  A round of workgroups starts and ends in
+// 2, 3, 4.5 and 9, the large tile in 26 where the value before the activation is kept: the epilogue and the stores of two
+// workgroups on a compute unit pass beneath the other one's products, the large tile has nobody.  Splits: a launch and the
+// traffic of their partial sums.
 static double rounds_of(int64_t n, double deep, int per_cu, const double (&stage)[3], double ends) {
   const int64_t places = 256 * per_cu, full = n / places, rest = n % places;
   double t = (double)full * (deep * stage[per_cu - 1] + ends);
   if (rest) t += deep * stage[rest <= 256 ? 0 : (rest <= 512 ? 1 : 2)] + ends;
   return t;
 }
-static const double kStage64[3] = {0.33, 0.46, 0.60}, kStage128[3] = {0.62, 0.96, 0.96}, kStage192[3] = {0.80, 1.19, 1.19},
-                    kStage256[3] = {1.50, 1.50, 1.50}, kStageF32[3] = {2.0, 2.5, 3.0};
+static const double kStage64[3] = {0.33, 0.46, 0.60}, kStage128[3] = {0.62, 0.96, 0.96}, kStage192[3] = {0.80, 1.23, 1.23},
+                    kStage256[3] = {1.67, 1.67, 1.67}, kStageF32[3] = {2.0, 2.5, 3.0};
 
-// What takes the least time by the figures above.  16384 rows of 1024 -> 4096 with GELU and pre kept: 256 x 256 221, bands of 192
-// rows 190, with the last 1024 rows in bands of 128 (which fill the last round) 182; 4096 -> 4096: 256 x 256 456, bands 481.
-// 1024 rows of 1024 -> 1024: 64 x 64 9.5, 128 x 128 13.5; 4096 rows: 19 and 15.  128 rows of 4096 -> 512: one split 25, eight 10.
-LinearPlan plan_linear(int64_t M, int64_t N, int64_t K, bool bf16, bool, bool, bool dbias) {
+// What takes the least time by the figures above.  16384 rows of 1024 -> 4096 with GELU and pre kept: 256 x 256 222, bands of 192
+// rows 182; without either 146 and 149; 4096 -> 4096: 256 x 256 466, bands 494.  1024 rows of 1024 -> 1024: 64 x 64 9.5,
+// 128 x 128 13.5; 4096 rows: 19 and 15.  128 rows of 4096 -> 512: one split 25, eight 10.
+LinearPlan plan_linear(int64_t M, int64_t N, int64_t K, bool bf16, bool by_depth, bool keeps, bool dbias) {
   static const int kSplits[] = {1, 2, 3, 4, 6, 8, 12, 16, 24, 32, 48, 64};
   auto count = [](int64_t x, int64_t t) { return (x + t - 1) / t; };
   const int64_t stages = count(K, kDepth), n64 = count(M, 64) * count(N, 64), cols = count(N, 128), n128 = count(M, 128) * cols,
@@ -342,18 +369,19 @@ LinearPlan plan_linear(int64_t M, int64_t N, int64_t K, bool bf16, bool, bool, b
     const int64_t slice = count(stages, s);
     if (s > 1 && (s > stages || s * M * N > ((int64_t)32 << 20) || n64 * s > 4096)) break;
     if (count(stages, slice) != s) continue;                                // every split gets at least one stage
-    const double deep = (double)slice, join = s > 1 ? 2.6 + (double)(2 * s + 1) * (double)(M * N) * 4.0 / 5.5e6 : 0.0;
+    const double deep = (double)slice, small_deep = by_depth ? 1.17 * deep : deep;
+    const double join = s > 1 ? 3.5 + (double)(2 * s + 1) * (double)(M * N) * 4.0 / 5.5e6 : 0.0;
     auto consider = [&](int tile, int64_t high, int64_t low, double cost) {
       cost += join;
       if (best.tile && cost >= best_cost) return;
       best_cost = cost;
       best.tile = tile; best.high = (int)high; best.low = (int)low; best.splits = s; best.slice = slice * kDepth;
     };
-    if (n64 <= 4096 || !bf16) consider(64, 0, 0, rounds_of(n64 * s, deep, 3, bf16 ? kStage64 : kStageF32, 2.0));
-    if (!bf16 || n64 <= 256) continue;
-    consider(128, 0, count(M, 128), rounds_of(n128 * s, deep, 2, kStage128, 3.0));
-    if (n256 * s >= 128) consider(256, 0, 0, rounds_of(n256 * s, deep, 1, kStage256, 20.0));
-    if (s > 1 || n128 <= 512) continue;
+    if (n64 <= 4096 || !bf16) consider(64, 0, 0, rounds_of(n64 * s, small_deep, 3, bf16 ? kStage64 : kStageF32, 2.0));
+    if (!bf16 || n64 <= 64) continue;
+    consider(128, 0, count(M, 128), rounds_of(n128 * s, small_deep, 2, kStage128, 3.0));
+    if (n256 * s >= 64) consider(256, 0, 0, rounds_of(n256 * s, deep, 1, kStage256, keeps ? 26.0 : 9.0));
+    if (s > 1 || n128 <= 512 || by_depth) continue;
     // whole rounds of 192-row bands, or what leaves up to 24 bands of 128 rows for the last one
     for (int64_t low = 0; low <= 24 && low * 128 < M; ++low) {
       const int64_t high = count(M - low * 128, 192);

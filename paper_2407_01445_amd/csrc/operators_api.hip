@@ -71,18 +71,18 @@ static LinearArgs linear_args(const fastclip_linear_config& c, int32_t pass) {
   }
   return a;
 }
-static LinearPlan plan_of(const LinearArgs& a, int32_t pass) {
-  return plan_linear(a.M, a.N, a.K, a.bf16, a.p_by_depth, a.q_by_depth, pass == FASTCLIP_LINEAR_BACKWARD_WEIGHT);
+static LinearPlan plan_of(const LinearArgs& a, bool keeps) {
+  return plan_linear(a.M, a.N, a.K, a.bf16, a.p_by_depth, keeps, a.p_by_depth);
 }
 
-static fastclip_status run_linear(LinearArgs& a, int32_t pass, void* workspace, size_t workspace_bytes, void* stream) {
+static fastclip_status run_linear(LinearArgs& a, void* workspace, size_t workspace_bytes, void* stream) {
   hipStream_t s = (hipStream_t)stream;
   if (a.M == 0) return FASTCLIP_OK;
   if (a.K == 0) {
     launch_linear_empty(a, s);
     return launch_status();
   }
-  const LinearPlan plan = plan_of(a, pass);
+  const LinearPlan plan = plan_of(a, a.pre_out != nullptr);
   if (((a.M + plan.tile - 1) / plan.tile) * ((a.N + plan.tile - 1) / plan.tile) * plan.splits > (1 << 23))
     return FASTCLIP_ERR_UNSUPPORTED;      // one launch
   if (plan.bytes) {
@@ -171,7 +171,9 @@ fastclip_status fastclip_layer_norm_backward(const fastclip_layer_norm_config* c
 size_t fastclip_linear_workspace_bytes(const fastclip_linear_config* cfg, int32_t pass) {
   if (fc::check(cfg, pass) != FASTCLIP_OK) return 0;
   const fc::LinearArgs a = fc::linear_args(*cfg, pass);
-  return a.M == 0 || a.K == 0 ? 0 : fc::plan_of(a, pass).bytes;
+  if (a.M == 0 || a.K == 0) return 0;
+  const size_t plain = fc::plan_of(a, false).bytes, keeps = pass == FASTCLIP_LINEAR_FORWARD ? fc::plan_of(a, true).bytes : 0;
+  return plain > keeps ? plain : keeps;
 }
 
 fastclip_status fastclip_linear_forward(const fastclip_linear_config* cfg, const void* x, const void* w, const float* bias,
@@ -188,7 +190,7 @@ fastclip_status fastclip_linear_forward(const fastclip_linear_config* cfg, const
   fc::LinearArgs a = fc::linear_args(*cfg, FASTCLIP_LINEAR_FORWARD);
   a.p = x; a.q = w; a.bias = bias; a.residual = residual; a.ld_res = cfg->ld_res; a.out = y; a.pre_out = pre;
   a.ld_pre = cfg->ld_pre;
-  return fc::run_linear(a, FASTCLIP_LINEAR_FORWARD, workspace, workspace_bytes, stream);
+  return fc::run_linear(a, workspace, workspace_bytes, stream);
 }
 
 fastclip_status fastclip_linear_backward_input(const fastclip_linear_config* cfg, const void* dy, const void* w, const void* pre,
@@ -203,7 +205,7 @@ fastclip_status fastclip_linear_backward_input(const fastclip_linear_config* cfg
     return FASTCLIP_ERR_UNSUPPORTED;
   fc::LinearArgs a = fc::linear_args(*cfg, FASTCLIP_LINEAR_BACKWARD_INPUT);
   a.p = dy; a.q = w; a.out = dx; a.pre_in = slope ? pre : nullptr; a.ld_pre = cfg->ld_pre;
-  return fc::run_linear(a, FASTCLIP_LINEAR_BACKWARD_INPUT, workspace, workspace_bytes, stream);
+  return fc::run_linear(a, workspace, workspace_bytes, stream);
 }
 
 fastclip_status fastclip_linear_backward_weight(const fastclip_linear_config* cfg, const void* dy, const void* x, void* dw,
@@ -216,7 +218,7 @@ fastclip_status fastclip_linear_backward_weight(const fastclip_linear_config* cf
     return FASTCLIP_ERR_UNSUPPORTED;
   fc::LinearArgs a = fc::linear_args(*cfg, FASTCLIP_LINEAR_BACKWARD_WEIGHT);
   a.p = dy; a.q = x; a.out = dw; a.dbias = dbias;
-  return fc::run_linear(a, FASTCLIP_LINEAR_BACKWARD_WEIGHT, workspace, workspace_bytes, stream);
+  return fc::run_linear(a, workspace, workspace_bytes, stream);
 }
 
 size_t fastclip_adamw_table_bytes(const fastclip_adamw_tensor* tensors, int64_t count) {
