@@ -353,7 +353,7 @@ static double rounds_of(int64_t n, double deep, int per_cu, const double (&stage
   return t;
 }
 static const double kStage64[3] = {0.33, 0.46, 0.60}, kStage128[3] = {0.62, 0.96, 0.96}, kStage192[3] = {0.80, 1.23, 1.23},
-                    kStage256[3] = {1.67, 1.67, 1.67}, kStageF32[3] = {2.0, 2.5, 3.0};
+                    kStage256[3] = {1.67, 1.67, 1.67}, kStageF32[3] = {0.40, 0.48, 0.48};
 
 // What takes the least time by the figures above.  16384 rows of 1024 -> 4096 with GELU and pre kept: 256 x 256 222, bands of 192
 // rows 182; without either 146 and 149; 4096 -> 4096: 256 x 256 466, bands 494.  1024 rows of 1024 -> 1024: 64 x 64 9.5,
@@ -377,8 +377,12 @@ LinearPlan plan_linear(int64_t M, int64_t N, int64_t K, bool bf16, bool by_depth
       best_cost = cost;
       best.tile = tile; best.high = (int)high; best.low = (int)low; best.splits = s; best.slice = slice * kDepth;
     };
-    if (n64 <= 4096 || !bf16) consider(64, 0, 0, rounds_of(n64 * s, small_deep, 3, bf16 ? kStage64 : kStageF32, 2.0));
-    if (!bf16 || n64 <= 64) continue;
+    if (!bf16) {
+      consider(32, 0, 0, rounds_of(count(M, 32) * count(N, 32) * s, deep, 2, kStageF32, 1.5));
+      continue;
+    }
+    if (n64 <= 4096) consider(64, 0, 0, rounds_of(n64 * s, small_deep, 3, kStage64, 2.0));
+    if (n64 <= 64) continue;
     consider(128, 0, count(M, 128), rounds_of(n128 * s, small_deep, 2, kStage128, 3.0));
     if (n256 * s >= 64) consider(256, 0, 0, rounds_of(n256 * s, deep, 1, kStage256, keeps ? 26.0 : 9.0));
     if (s > 1 || n128 <= 512 || by_depth) continue;

@@ -3,144 +3,204 @@
 //
 //   out[m, n] = sum_k P[m, k] Q[n, k]
 //
-// A workgroup of four wavefronts forms a 64 x 64 tile, 32 of k a stage: the next stage comes into registers while the matrix
-// cores work on the present one in LDS, guarded, so that what lies outside the matrices is zero.  The order of k inside a stage
-// is free as long as both operands keep to it: lanes below 32 take k = 8 s .. 8 s + 3, the others 8 s + 4 .. 8 s + 7, which an
-// operand by rows reads as 16 bytes for four products.  P gives the MFMA's rows, so that 32 lanes hold neighbouring columns and
-// a store is whole lines whatever the alignment.
+// The fp32 matrix cores take 64 cycles for the 128 operand words of a product, so that one wavefront needs little data at a time,
+// and wavefronts need not meet: four of them share a tile by taking every fourth block of 32 of k (a line of an operand by rows),
+// each with two blocks of LDS of its own, the next one on its way from memory by direct-to-LDS loads while the present one is
+// multiplied.  There is no barrier until they add up, each then finishing a quarter of the tile.  (Operands straight from memory
+// into registers instead, as the products want them, fetch 32 bytes of each of 32 lines per load and took twice as long.)  The
+// order of k inside a block is free as long as both operands keep to it: lanes below 32 take k = 8 s .. 8 s + 3, the others
+// 8 s + 4 .. 8 s + 7, which by rows is one 16-byte read for four products.  P gives the MFMA's rows, so that 32 lanes hold
+// neighbouring columns and a store is whole lines whatever the alignment.
+//
+// Edges: rows beyond M (columns beyond N) repeat the last one, and what they produce is not stored; depth beyond K comes from a
+// block of zeros.
 #include "linear_common.hpp"
 
 namespace fc {
 
-constexpr int kTile32 = 64, kDepth32 = 32;
-constexpr int kRowFloats = 36;      // by rows: 32 of k and 4 more, so that the 16 rows of a read cover the banks
-constexpr int kDepthFloats = 72;    // by depth: 64 columns and 8 more, so that rows of k four apart lie in different halves of the banks
-constexpr int kPanelFloats = 64 * kRowFloats;     // either layout
+constexpr int kBlock32 = 32;                     // of k
+constexpr uint32_t kPanel32 = 32 * 128;          // bytes of 32 rows (columns) of a block
+__device__ __align__(16) uint32_t g_zero_f32[4] = {0, 0, 0, 0};
 
-template <bool BY_DEPTH>
+// 4 or 16 bytes per lane from an address of its own into LDS
+template <bool WIDE>
+__device__ __forceinline__ void dma_from(const void* lane_address, uint32_t lds_byte_addr) {
+  if constexpr (WIDE)
+    asm volatile("s_mov_b32 m0, %1\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %0, off"
+                 : : "v"(lane_address), "s"(__builtin_amdgcn_readfirstlane(lds_byte_addr)) : "memory");
+  else
+    asm volatile("s_mov_b32 m0, %1\n\ts_nop 0\n\tglobal_load_lds_dword %0, off"
+                 : : "v"(lane_address), "s"(__builtin_amdgcn_readfirstlane(lds_byte_addr)) : "memory");
+}
+
+typedef float Words32[4][4];       // [s][j]: k = 8 s + 4 h + j of a row (column)
+
+// 32 rows (columns) of an operand from `first` on.  LDS image by rows: 128 bytes a row, 16-byte chunk c of
+// row r at c ^ ((r >> 1) & 7); by depth: 128 bytes a row of k, row k at k ^ ((k >> 2) & 1), so that the rows k and k + 4 that the
+// halves of a wavefront read lie in different halves of the banks.  WIDE: 16 bytes a lane and load, else 4.
+template <bool BY_DEPTH, bool WIDE>
 struct Operand32 {
-  const float* base;
-  int64_t ld;
-  int left;            // rows (columns) of the tile that exist
-  bool wide;           // 16-byte loads
-  int tid;
-  float r[2][4];
-  __device__ __forceinline__ void open(const void* matrix, int64_t ld_, int64_t first, int64_t count, int tid_) {
-    ld = ld_; tid = tid_;
-    base = (const float*)matrix + (BY_DEPTH ? first : first * ld);
-    left = (int)(count - first < kTile32 ? count - first : kTile32);
-    wide = !((uintptr_t)matrix & 15) && ld % 4 == 0;
+  static constexpr int kLoads = WIDE ? 4 : 16;     // wave loads of a block of k
+  const char* base;                // wave-uniform
+  int64_t line;                    // bytes from one row (row of k) to the next
+  uint32_t off[kLoads];            // this lane's bytes from there at depth 0
+  int lane;
+  // k of this lane's (first) word of load i, inside a block
+  __device__ __forceinline__ int depth_of(int i) const {
+    const int r = WIDE ? 8 * i + (lane >> 3) : 2 * i + (lane >> 5);
+    if constexpr (BY_DEPTH) return r ^ ((r >> 2) & 1);
+    if constexpr (WIDE) return 4 * ((lane & 7) ^ ((r >> 1) & 7));
+    return 4 * (((lane >> 2) & 7) ^ ((r >> 1) & 7)) + (lane & 3);
   }
-  __device__ __forceinline__ void request(int64_t k0, int64_t end) {
+  __device__ __forceinline__ void open(const void* matrix, int64_t ld, int64_t first, int64_t count, int lane_) {
+    line = ld * 4; lane = lane_;
+    base = wave_uniform((const char*)matrix + (BY_DEPTH ? first * 4 : first * line));
+    const int left = (int)(count - first < 32 ? count - first : 32);
 #pragma unroll
-    for (int i = 0; i < 2; ++i) {
-      // four words of this thread: columns c .. c + 3 of line `line` (a row, or a row of k)
-      const int line = BY_DEPTH ? (tid >> 4) + 16 * i : (tid >> 3) + 32 * i;
-      const int c = BY_DEPTH ? (tid & 15) * 4 : (tid & 7) * 4;
-      const float* at = base + (BY_DEPTH ? (k0 + line) * ld + c : line * ld + k0 + c);
-      const bool in = BY_DEPTH ? k0 + line < end : line < left;
-      const int64_t rest = BY_DEPTH ? left - c : end - k0 - c;      // words from c on that exist
-      if (in && wide && rest >= 4) {
-        const float4 v = *(const float4*)at;
-        r[i][0] = v.x; r[i][1] = v.y; r[i][2] = v.z; r[i][3] = v.w;
+    for (int i = 0; i < kLoads; ++i) {
+      int r;                       // row, or column (the first of four)
+      if constexpr (BY_DEPTH) {
+        r = WIDE ? 4 * (lane & 7) : lane & 31;
+        r = r < left ? r : left - (WIDE ? 4 : 1);
+        off[i] = (uint32_t)depth_of(i) * (uint32_t)line + (uint32_t)r * 4u;
       } else {
-#pragma unroll
-        for (int e = 0; e < 4; ++e) r[i][e] = in && e < rest ? at[e] : 0.f;
+        r = WIDE ? 8 * i + (lane >> 3) : 2 * i + (lane >> 5);
+        r = r < left ? r : left - 1;
+        off[i] = (uint32_t)r * (uint32_t)line + (uint32_t)depth_of(i) * 4u;
       }
     }
   }
-  __device__ __forceinline__ void deposit(float* panel) const {
+  // requests the block of k from k0 on (wave-uniform)
+  __device__ __forceinline__ void request(int64_t k0, int64_t end, uint32_t lds) const {
+    const char* at = base + (BY_DEPTH ? k0 * line : k0 * 4);
+    constexpr uint32_t kStep = WIDE ? 1024 : 256;
+    if (k0 + kBlock32 <= end) {
 #pragma unroll
-    for (int i = 0; i < 2; ++i) {
-      const int line = BY_DEPTH ? (tid >> 4) + 16 * i : (tid >> 3) + 32 * i;
-      const int c = BY_DEPTH ? (tid & 15) * 4 : (tid & 7) * 4;
-      *(float4*)(panel + line * (BY_DEPTH ? kDepthFloats : kRowFloats) + c) = make_float4(r[i][0], r[i][1], r[i][2], r[i][3]);
+      for (int i = 0; i < kLoads; ++i) {
+        if constexpr (WIDE) dma16(at, off[i], lds + (uint32_t)i * kStep);
+        else dma4(at, off[i], lds + (uint32_t)i * kStep);
+      }
+    } else {
+#pragma unroll
+      for (int i = 0; i < kLoads; ++i)
+        dma_from<WIDE>(k0 + depth_of(i) < end ? at + off[i] : (const char*)g_zero_f32, lds + (uint32_t)i * kStep);
     }
   }
-  // k = 8 s + 4 h .. + 3 of row (column) `at`
-  static __device__ __forceinline__ void read(const float* panel, int at, int h, int s, float (&x)[4]) {
-    if constexpr (BY_DEPTH) {
+  static __device__ __forceinline__ void read(Words32& x, const char* panel, int lr, int h) {
 #pragma unroll
-      for (int j = 0; j < 4; ++j) x[j] = panel[(8 * s + 4 * h + j) * kDepthFloats + at];
-    } else {
-      const float4 v = *(const float4*)(panel + at * kRowFloats + 8 * s + 4 * h);
-      x[0] = v.x; x[1] = v.y; x[2] = v.z; x[3] = v.w;
+    for (int s = 0; s < 4; ++s) {
+      if constexpr (BY_DEPTH) {
+#pragma unroll
+        for (int j = 0; j < 4; ++j) {
+          const int k = 8 * s + 4 * h + j;
+          x[s][j] = *(const float*)(panel + (k ^ ((k >> 2) & 1)) * 128 + lr * 4);
+        }
+      } else {
+        const float4 v = *(const float4*)(panel + lr * 128 + (((2 * s + h) ^ ((lr >> 1) & 7)) << 4));
+        x[s][0] = v.x; x[s][1] = v.y; x[s][2] = v.z; x[s][3] = v.w;
+      }
     }
   }
 };
 
-template <bool PD, bool QD>
-__global__ void __launch_bounds__(256) k_linear_f32(LinearArgs a, uint32_t tiles_m, uint32_t tiles_n, int64_t slice) {
-  __shared__ __attribute__((aligned(16))) float panels[2][2][kPanelFloats];
-  const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6, wm = wave & 1, wn = wave >> 1, lr = lane & 31, hk = lane >> 5;
-  const TilePlace place = tile_place(blockIdx.x, gridDim.x, tiles_m, tiles_n);
-  const int64_t m0 = place.m * kTile32, n0 = place.n * kTile32, k0 = place.split * slice;
+template <bool PD, bool QD, bool WIDE>
+__global__ void __launch_bounds__(256) k_linear_f32(LinearArgs a, uint32_t rows, uint32_t cols, int splits, int64_t slice) {
+  typedef Operand32<PD, WIDE> OpP;
+  typedef Operand32<QD, WIDE> OpQ;
+  constexpr uint32_t kBuffer = 2 * kPanel32;
+  constexpr int kRequests = OpP::kLoads + OpQ::kLoads;
+  __shared__ __attribute__((aligned(1024))) char ring[4 * 2 * kBuffer];      // per wavefront two blocks; then the parts of the sums
+  const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6), lr = lane & 31, hk = lane >> 5;
+  const TilePlace place = tile_place(blockIdx.x, gridDim.x, rows, cols);
+  const int64_t m0 = place.m * 32, n0 = place.n * 32, k0 = place.split * slice;
   const int64_t end = k0 + slice < a.K ? k0 + slice : a.K;
-  const int stages = (int)((end - k0 + kDepth32 - 1) / kDepth32);
-  Operand32<PD> p;
-  Operand32<QD> q;
-  p.open(a.p, a.ldp, m0, a.M, tid);
-  q.open(a.q, a.ldq, n0, a.N, tid);
-  f32x16 acc;
+  OpP p;
+  OpQ q;
+  p.open(a.p, a.ldp, m0, a.M, lane);
+  q.open(a.q, a.ldq, n0, a.N, lane);
+  f32x16 acc[2];               // two chains of sums: a product does not wait for the one in front
 #pragma unroll
-  for (int v = 0; v < 16; ++v) acc[v] = 0.f;
-  const bool sums = PD && QD && a.dbias && place.n == 0 && wn == 0;
+  for (int i = 0; i < 2; ++i)
+#pragma unroll
+    for (int v = 0; v < 16; ++v) acc[i][v] = 0.f;
+  const bool sums = PD && QD && a.dbias && place.n == 0;      // this tile also sums P over the depth
   float total = 0.f;
 
-  p.request(k0, end);
-  q.request(k0, end);
-  p.deposit(panels[0][0]);
-  q.deposit(panels[0][1]);
+  constexpr int64_t kStep = 4 * kBlock32;
+  const char* mine = ring + wave * 2 * kBuffer;
+  const uint32_t mine_at = lds_addr(mine);
+  auto request = [&](int64_t k, uint32_t buffer) {
+    p.request(k, end, mine_at + buffer);
+    q.request(k, end, mine_at + buffer + kPanel32);
+  };
+  uint32_t here = 0;
+  if (k0 + wave * kBlock32 < end) request(k0 + wave * kBlock32, 0);
+  for (int64_t k = k0 + wave * kBlock32; k < end; k += kStep) {
+    if (k + kStep < end) {
+      request(k + kStep, here ^ kBuffer);
+      wait_vmcnt<kRequests>();                   // the older block's have landed
+    } else {
+      FC_WAIT_VMCNT0();
+    }
+    FC_FENCE();
+    __builtin_amdgcn_wave_barrier();
+    Words32 x, y;
+    OpP::read(x, mine + here, lr, hk);
+    OpQ::read(y, mine + here + kPanel32, lr, hk);
+#pragma unroll
+    for (int s = 0; s < 4; ++s)
+#pragma unroll
+      for (int j = 0; j < 4; ++j) acc[j & 1] = __builtin_amdgcn_mfma_f32_32x32x2f32(x[s][j], y[s][j], acc[j & 1], 0, 0, 0);
+    if constexpr (PD && QD) {
+      if (sums) {
+        float some = 0.f;
+#pragma unroll
+        for (int s = 0; s < 4; ++s) some += (x[s][0] + x[s][1]) + (x[s][2] + x[s][3]);
+        total += some;
+      }
+    }
+    FC_FENCE();                                  // the block's reads are over before the next request takes its place
+    __builtin_amdgcn_wave_barrier();
+    here ^= kBuffer;
+  }
+
   __syncthreads();
-  for (int g = 0; g < stages; ++g) {
-    const bool more = g + 1 < stages;
-    if (more) {
-      p.request(k0 + (int64_t)(g + 1) * kDepth32, end);
-      q.request(k0 + (int64_t)(g + 1) * kDepth32, end);
-    }
-    const float* panel_p = panels[g & 1][0];
-    const float* panel_q = panels[g & 1][1];
-    float some = 0.f;
-#pragma unroll
-    for (int s = 0; s < kDepth32 / 8; ++s) {
-      float x[4], y[4];
-      Operand32<PD>::read(panel_p, wm * 32 + lr, hk, s, x);
-      Operand32<QD>::read(panel_q, wn * 32 + lr, hk, s, y);
-#pragma unroll
-      for (int j = 0; j < 4; ++j) acc = __builtin_amdgcn_mfma_f32_32x32x2f32(x[j], y[j], acc, 0, 0, 0);
-      if constexpr (PD && QD) some += (x[0] + x[1]) + (x[2] + x[3]);
-    }
-    total += some;
-    if (more) {
-      p.deposit(panels[(g + 1) & 1][0]);
-      q.deposit(panels[(g + 1) & 1][1]);
+  float(*parts)[16][64] = (float(*)[16][64])ring;
+  if (sums) {
+    parts[wave][0][lane] = total + __shfl_xor(total, 32);
+    __syncthreads();
+    if (tid < 32 && m0 + tid < a.M) {
+      float* to = splits > 1 ? a.partial + (int64_t)splits * a.M * a.N + (int64_t)place.split * a.M : a.dbias;
+      to[m0 + tid] = (parts[0][0][tid] + parts[1][0][tid]) + (parts[2][0][tid] + parts[3][0][tid]);
     }
     __syncthreads();
   }
-
-  const bool split = gridDim.x > tiles_m * tiles_n;
-  if (sums) {
-    const float s = total + __shfl_xor(total, 32);
-    const int64_t m = m0 + wm * 32 + lr;
-    float* to = split ? a.partial + (int64_t)(gridDim.x / (tiles_m * tiles_n)) * a.M * a.N + place.split * a.M : a.dbias;
-    if (hk == 0 && m < a.M) to[m] = s;
-  }
-  const int64_t n = n0 + wn * 32 + lr;
 #pragma unroll
-  for (int v = 0; v < 16; ++v) {
-    const int64_t m = m0 + wm * 32 + 8 * (v >> 2) + 4 * hk + (v & 3);
+  for (int v = 0; v < 16; ++v) parts[wave][v][lane] = acc[0][v] + acc[1][v];
+  __syncthreads();
+  // this wavefront finishes the accumulators number v with v mod 4 its own
+#pragma unroll
+  for (int t = 0; t < 4; ++t) {
+    const int v = 4 * t + wave;
+    const int64_t m = m0 + 8 * (v >> 2) + 4 * hk + (v & 3), n = n0 + lr;
+    float z[1] = {(parts[0][v][lane] + parts[1][v][lane]) + (parts[2][v][lane] + parts[3][v][lane])};
     if (m < a.M && n < a.N) {
-      float z[1] = {acc[v]};
-      if (split) a.partial[((int64_t)place.split * a.M + m) * a.N + n] = z[0];
+      if (splits > 1) a.partial[((int64_t)place.split * a.M + m) * a.N + n] = z[0];
       else finish_values<false, 1>(a, z, m, n);
     }
   }
 }
 
+// 16-byte loads: aligned lines of whole words, also at an operand's edges (by rows the depth, by depth the columns)
+static bool wide_f32(const void* p, int64_t ld, int64_t width) { return !((uintptr_t)p & 15) && ld % 4 == 0 && width % 4 == 0; }
+
 template <bool PD, bool QD>
 static void launch_form_f32(const LinearArgs& a, const LinearPlan& plan, hipStream_t s) {
-  const uint32_t tm = (uint32_t)((a.M + kTile32 - 1) / kTile32), tn = (uint32_t)((a.N + kTile32 - 1) / kTile32);
-  hipLaunchKernelGGL((k_linear_f32<PD, QD>), dim3(tm * tn * (uint32_t)plan.splits), dim3(256), 0, s, a, tm, tn, plan.slice);
+  const uint32_t rows = (uint32_t)((a.M + 31) / 32), cols = (uint32_t)((a.N + 31) / 32);
+  const dim3 grid(rows * cols * (uint32_t)plan.splits);
+  const bool wide = wide_f32(a.p, a.ldp, PD ? a.M : a.K) && wide_f32(a.q, a.ldq, QD ? a.N : a.K);
+  if (wide) hipLaunchKernelGGL((k_linear_f32<PD, QD, true>), grid, dim3(256), 0, s, a, rows, cols, plan.splits, plan.slice);
+  else hipLaunchKernelGGL((k_linear_f32<PD, QD, false>), grid, dim3(256), 0, s, a, rows, cols, plan.splits, plan.slice);
 }
 
 void launch_linear_f32(const LinearArgs& a, const LinearPlan& plan, hipStream_t s) {

@@ -31,7 +31,9 @@ def _asm_replacement(m):
     t = m.group(0)
     if "s_add_u32 m0" in t:                      # 16 bytes per lane into LDS at (uniform + IMM) + 16 lane
         return "emu_dma(uniform_base, lane_byte_off, lds_uniform + (uint32_t)IMM, 16);"
-    if "global_load_lds_dwordx4 %0, off" in t:   # ... from an address of the lane's own
+    if "global_load_lds_dword %0, off" in t:     # from an address of the lane's own
+        return "emu_dma(lane_address, 0, lds_byte_addr, 4);"
+    if "global_load_lds_dwordx4 %0, off" in t:
         return "emu_dma(lane_address, 0, lds_byte_addr, 16);"
     if "global_load_lds_dwordx4" in t:
         return "emu_dma(uniform_base, lane_byte_off, lds_byte_addr, 16);"
