@@ -96,6 +96,7 @@ class fastclip_adamw_table(C.Structure):
 
 
 _lib = None
+_torch = None
 
 
 def load(build_if_missing: bool = True):
@@ -254,11 +255,17 @@ def _stream(stream):
 def _current_stream() -> int:
     """Address of torch's current stream on the current device.  torch.cuda.current_stream() builds an object around it, 3.4 us
     a call and a third of a small step's time on the host; torch's own raw lookup takes 0.2."""
-    import torch
-    raw, device = getattr(torch._C, "_cuda_getCurrentRawStream", None), getattr(torch._C, "_cuda_getDevice", None)
-    if raw is None or device is None or not torch.cuda.is_initialized():
-        return torch.cuda.current_stream().cuda_stream
-    return raw(device())
+    global _torch
+    if _torch is None:
+        import torch
+        _torch = torch
+    try:
+        if _torch.cuda.is_initialized():
+            c = _torch._C
+            return c._cuda_getCurrentRawStream(c._cuda_getDevice())
+    except AttributeError:
+        pass
+    return _torch.cuda.current_stream().cuda_stream
 
 
 def fastclip_workspace_bytes(cfg: fastclip_config) -> int:
@@ -512,30 +519,31 @@ def make_adamw_tensor(*, param, grad, m, v, param_bf16=None, weight_decay=0.0, m
     """Contiguous CUDA tensors of one size: param fp32, grad fp32 or bf16, m and v fp32 or uint8 (then with the blocks'
     exponents).  The struct keeps them referenced."""
     n = param.numel()
-    held = [t for t in (param, grad, m, v, param_bf16, m_exp, v_exp) if t is not None]
-    if not all(t.is_contiguous() for t in held):
-        raise ValueError("adamw tensors must be contiguous")
-    if any(t is not None and t.numel() != n for t in (grad, m, v, param_bf16)):
-        raise ValueError("param, grad, m, v and param_bf16 must have the same number of elements")
-    if any(t is not None and t.numel() != -(-n // ADAMW_BLOCK) for t in (m_exp, v_exp)):
-        raise ValueError("an exponent for every block of %d elements" % ADAMW_BLOCK)
-    out = fastclip_adamw_tensor(_ptr(param), _ptr(grad), _ptr(m), _ptr(v), _ptr(param_bf16), _ptr(m_exp), _ptr(v_exp), n,
-                                float(weight_decay), 0)
-    out._keepalive = held
-    out._types = tuple(None if t is None else str(t.dtype) for t in (param, grad, m, v, param_bf16, m_exp, v_exp))
+    parts = (param, grad, m, v, param_bf16, m_exp, v_exp)
+    for i, t in enumerate(parts):
+        if t is None:
+            continue
+        if not t.is_contiguous():
+            raise ValueError("adamw tensors must be contiguous")
+        if t.numel() != (n if i < 5 else -(-n // ADAMW_BLOCK)):
+            raise ValueError("param, grad, m, v and param_bf16 must have the same number of elements" if i < 5 else
+                             "an exponent for every block of %d elements" % ADAMW_BLOCK)
+    out = fastclip_adamw_tensor(*map(_ptr, parts), n, weight_decay, 0)
+    out._keepalive, out._types = parts, tuple(None if t is None else t.dtype for t in parts)
     return out
 
 
 def make_adamw_table(cfg, tensors) -> fastclip_adamw_table:
     """The device table of a list of make_adamw_tensor()s, for every later step on them; keeps them referenced."""
     import torch
-    grad = {BF16: "torch.bfloat16", F32: "torch.float32"}.get(cfg.grad_dtype)
-    state, exps = ("torch.uint8", "torch.uint8") if cfg.state_bits == 8 else ("torch.float32", None)
+    grad = {BF16: torch.bfloat16, F32: torch.float32}.get(cfg.grad_dtype)
+    state, exps = (torch.uint8, torch.uint8) if cfg.state_bits == 8 else (torch.float32, None)
+    want = (torch.float32, grad, state, state, torch.bfloat16, exps, exps)
+    allowed = {want, want[:4] + (None,) + want[5:]}              # the bf16 copy is optional; exponents with 32 bits are not looked at
     for t in tensors:
-        want = ("torch.float32", grad, state, state, "torch.bfloat16", exps, exps)
-        for have, wanted, optional in zip(t._types, want, (False, False, False, False, True, False, False)):
-            if wanted is not None and have != wanted and not (optional and have is None):
-                raise TypeError("adamw tensor of type %s where %s is wanted" % (have, wanted))
+        types = t._types if cfg.state_bits == 8 else t._types[:5] + (None, None)
+        if types not in allowed:
+            raise TypeError("adamw tensors of types %s where %s are wanted" % (types, want))
     lib, n = load(), len(tensors)
     array = (fastclip_adamw_tensor * max(1, n))(*tensors)
     nbytes = int(lib.fastclip_adamw_table_bytes(array, n))
@@ -544,9 +552,8 @@ def make_adamw_table(cfg, tensors) -> fastclip_adamw_table:
     st = int(lib.fastclip_adamw_table_fill(C.byref(cfg), array, n, host.data_ptr(), nbytes, C.byref(table)))
     if st != OK:
         raise FastclipError(st)
-    device = next((k.device for t in tensors for k in t._keepalive), None)
-    if device is not None and table.chunks:
-        room = host.to(device)                 # from pageable memory: complete when the call returns
+    if table.chunks:
+        room = host.to(tensors[0]._keepalive[0].device)       # from pageable memory: complete when the call returns
         table.device = room.data_ptr()
         table._keepalive = (room, [t._keepalive for t in tensors])
     return table

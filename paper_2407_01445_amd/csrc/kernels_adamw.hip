@@ -21,8 +21,14 @@ struct AdamwScalars {
 __device__ __forceinline__ AdamwScalars adamw_scalars(const AdamwArgs& a, float weight_decay) {
   return {a.beta1, a.beta2, 1.f - a.beta1, 1.f - a.beta2, a.step_size, a.corr2, a.eps, a.lr * weight_decay};
 }
+// Root and reciprocal as the hardware has them, an ulp each, of a step that is small beside p; the root's argument is lifted out of
+// the denormals, which the instruction does not take.
 __device__ __forceinline__ float adamw_move(float p, float m, float v, const AdamwScalars& k) {
-  return p - fmaf(p, k.decay, (m * k.step_size) / (sqrtf(v * k.corr2) + k.eps));
+  const float w = v * k.corr2;
+  const bool tiny = w < 0x1p-96f;
+  float s = __builtin_amdgcn_sqrtf(tiny ? w * 0x1p64f : w);
+  s = tiny ? s * 0x1p-32f : s;
+  return p - fmaf(p, k.decay, m * k.step_size * __builtin_amdgcn_rcpf(s + k.eps));
 }
 // b1 m + (1 - b1) g with one rounding of the sum and none of its terms: where they cancel, the first moment is all there is of p's
 // step, and two more instructions do not show beside the memory traffic
@@ -144,114 +150,125 @@ __device__ __forceinline__ int block_exponent(uint32_t hi) {      // of a block'
   return k < -94 ? -94 : (k > 126 ? 126 : k);
 }
 __device__ __forceinline__ uint32_t larger(uint32_t x, uint32_t y) { return x > y ? x : y; }
-__device__ __forceinline__ uint32_t wave_largest(uint32_t x) {
+struct Adamw8Scalars {
+  AdamwScalars k;
+  double b1, b2, c1, c2;       // the betas times what lifts a code out of fp32's denormals, without the block's 2^k; 1 - beta
+  uint32_t key;
+};
+// A block of a wavefront, four elements a lane: p and the codes in, new ones out; exponents as their bytes.  i: place of the
+// lane's first element in its tensor.
+__device__ __forceinline__ void adamw_8_block(const Adamw8Scalars& c, uint32_t i, const float (&g)[4], float (&p)[4], uint32_t& mc,
+                                              uint32_t& vc, uint32_t& m_exp, uint32_t& v_exp) {
+  // 2^(byte - 127) times the constants: the exponent field of a double stepped up
+  const double fm = c.b1 * pow2((int)m_exp - 127), fv = c.b2 * pow2((int)v_exp - 127);
+  double me[4], ve[4];
+  uint32_t tm = 0, tv = 0;
 #pragma unroll
-  for (int s = 32; s > 0; s >>= 1) x = larger(x, __shfl_xor(x, s));
-  return x;
+  for (int q = 0; q < 4; ++q) {
+    const uint32_t mq = (mc >> (8 * q)) & 255u, vq = (vc >> (8 * q)) & 255u;
+    const double x = (double)g[q];
+    me[q] = fma((double)__uint_as_float((mq & 127u) << 20 | (mq & 128u) << 24), fm, x * c.c1);
+    ve[q] = fma((double)__uint_as_float(vq << 20), fv, x * x * c.c2);
+    const uint32_t hm = upper_half(me[q]) & 0x7fffffffu, hv = upper_half(ve[q]) & 0x7fffffffu;
+    tm = hm > tm ? hm : tm;
+    tv = hv > tv ? hv : tv;
+    p[q] = adamw_move(p[q], (float)me[q], (float)ve[q], c.k);
+  }
+  const int km = block_exponent(wave_largest(tm)), kv = block_exponent(wave_largest(tv));
+  m_exp = (uint32_t)(km + 127);
+  v_exp = (uint32_t)(kv + 127);
+  mc = vc = 0;
+#pragma unroll
+  for (int q = 0; q < 4; ++q) {
+    const uint32_t r = adamw_mix((i + q) ^ c.key);
+    const uint32_t hm = upper_half(me[q]), hv = upper_half(ve[q]) & 0x7fffffffu;
+    const uint32_t cm = adamw_code<kFirstTop>(hm & 0x7fffffffu, km + 1023, r & 0xffffu) | (me[q] < 0.0 ? 128u : 0u);
+    uint32_t cv = adamw_code<kSecondTop>(hv, kv + 1023, r >> 16);
+    cv = cv == 0 && ve[q] > 0.0 ? 1u : cv;
+    mc |= cm << (8 * q);
+    vc |= cv << (8 * q);
+  }
 }
 
-// A wavefront takes a block, four elements a lane.
+// A wavefront takes four blocks of a chunk.
 template <bool BF16>
 __global__ void __launch_bounds__(256) k_adamw_8(AdamwArgs a) {
   const AdamwChunk where = a.chunks[blockIdx.x];
   const AdamwEntry& e = a.entries[where.tensor];
   const int64_t n = e.n;
-  const AdamwScalars k = adamw_scalars(a, e.weight_decay);
-  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+  const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   float* __restrict__ p = e.param;
   uint8_t* __restrict__ m = (uint8_t*)e.m;
   uint8_t* __restrict__ v = (uint8_t*)e.v;
+  uint8_t* __restrict__ m_exp = e.m_exp;
+  uint8_t* __restrict__ v_exp = e.v_exp;
   const void* __restrict__ g = e.grad;
   uint16_t* __restrict__ copy = e.copy;
-  const uint32_t key = adamw_mix(a.seed + 0x9E3779B9u * (uint32_t)(where.tensor + 1));
-  const double b1 = (double)a.beta1, b2 = (double)a.beta2, c1 = 1.0 - b1, c2 = 1.0 - b2;
-  const bool wide = e.wide != 0;
-  float4 p4[4];
-  Grad4<BF16> g4[4];
-  uint32_t mw[4], vw[4];
-  int em[4], ev[4];
+  const Adamw8Scalars c = {adamw_scalars(a, e.weight_decay),
+                           (double)a.beta1 * pow2(127 - kFirstTop), (double)a.beta2 * pow2(127 - kSecondTop),
+                           1.0 - (double)a.beta1, 1.0 - (double)a.beta2,
+                           adamw_mix(a.seed + 0x9E3779B9u * (uint32_t)(where.tensor + 1))};
   const int64_t block0 = (int64_t)where.chunk * (kAdamwChunk / kAdamwBlock) + wave;     // this wavefront's: block0 + 4 j
+  if (e.wide && ((int64_t)where.chunk + 1) * kAdamwChunk <= n) {
+    float4 p4[4];
+    Grad4<BF16> g4[4];
+    uint32_t mw[4], vw[4], em[4], ev[4];
 #pragma unroll
-  for (int j = 0; j < 4; ++j) {
-    const int64_t block = block0 + 4 * j, i = block * kAdamwBlock + 4 * lane;
-    if (block * kAdamwBlock >= n) continue;      // the whole wavefront
-    em[j] = e.m_exp[block];
-    ev[j] = e.v_exp[block];
-    if (wide && (block + 1) * kAdamwBlock <= n) {
+    for (int j = 0; j < 4; ++j) {
+      const int64_t block = block0 + 4 * j, i = block * kAdamwBlock + 4 * lane;
+      em[j] = m_exp[block];
+      ev[j] = v_exp[block];
       p4[j] = *(const float4*)(p + i);
       g4[j].load(g, i);
       mw[j] = *(const uint32_t*)(m + i);
       vw[j] = *(const uint32_t*)(v + i);
     }
-  }
 #pragma unroll
-  for (int j = 0; j < 4; ++j) {
-    const int64_t block = block0 + 4 * j, i = block * kAdamwBlock + 4 * lane;
-    if (block * kAdamwBlock >= n) continue;
-    const bool whole = wide && (block + 1) * kAdamwBlock <= n;
-    float pe[4], ge[4];
-    uint32_t mc = mw[j], vc = vw[j];
-    if (whole) {
-      pe[0] = p4[j].x; pe[1] = p4[j].y; pe[2] = p4[j].z; pe[3] = p4[j].w;
+    for (int j = 0; j < 4; ++j) {
+      const int64_t block = block0 + 4 * j, i = block * kAdamwBlock + 4 * lane;
+      float pe[4] = {p4[j].x, p4[j].y, p4[j].z, p4[j].w}, ge[4];
 #pragma unroll
       for (int q = 0; q < 4; ++q) ge[q] = g4[j].get(q);
-    } else {
-      mc = vc = 0;
-#pragma unroll
-      for (int q = 0; q < 4; ++q) {
-        const bool in = i + q < n;
-        pe[q] = in ? p[i + q] : 0.f;
-        ge[q] = in ? grad_at<BF16>(g, i + q) : 0.f;
-        mc |= (in ? (uint32_t)m[i + q] : 0u) << (8 * q);
-        vc |= (in ? (uint32_t)v[i + q] : 0u) << (8 * q);
-      }
-    }
-    const double fm = b1 * pow2(127 - kFirstTop + em[j] - 127), fv = b2 * pow2(127 - kSecondTop + ev[j] - 127);
-    double me[4], ve[4];
-    uint32_t tm = 0, tv = 0;
-#pragma unroll
-    for (int q = 0; q < 4; ++q) {
-      const uint32_t mq = (mc >> (8 * q)) & 255u, vq = (vc >> (8 * q)) & 255u;
-      const double x = (double)ge[q];
-      me[q] = fma((double)__uint_as_float((mq & 127u) << 20 | (mq & 128u) << 24), fm, x * c1);
-      ve[q] = fma((double)__uint_as_float(vq << 20), fv, x * x * c2);
-      tm = larger(tm, upper_half(me[q]) & 0x7fffffffu);
-      tv = larger(tv, upper_half(ve[q]) & 0x7fffffffu);
-      pe[q] = adamw_move(pe[q], (float)me[q], (float)ve[q], k);
-    }
-    const int km = block_exponent(wave_largest(tm)), kv = block_exponent(wave_largest(tv));
-    mc = vc = 0;
-#pragma unroll
-    for (int q = 0; q < 4; ++q) {
-      const uint32_t r = adamw_mix((uint32_t)(i + q) ^ key);
-      const uint32_t hm = upper_half(me[q]), hv = upper_half(ve[q]) & 0x7fffffffu;
-      const uint32_t cm = adamw_code<kFirstTop>(hm & 0x7fffffffu, km + 1023, r & 0xffffu) | (me[q] < 0.0 ? 128u : 0u);
-      uint32_t cv = adamw_code<kSecondTop>(hv, kv + 1023, r >> 16);
-      cv = ve[q] > 0.0 && cv == 0 ? 1u : cv;
-      mc |= cm << (8 * q);
-      vc |= cv << (8 * q);
-    }
-    if (lane == 0) {
-      e.m_exp[block] = (uint8_t)(km + 127);
-      e.v_exp[block] = (uint8_t)(kv + 127);
-    }
-    if (whole) {
+      adamw_8_block(c, (uint32_t)i, ge, pe, mw[j], vw[j], em[j], ev[j]);
       *(float4*)(p + i) = make_float4(pe[0], pe[1], pe[2], pe[3]);
-      *(uint32_t*)(m + i) = mc;
-      *(uint32_t*)(v + i) = vc;
+      *(uint32_t*)(m + i) = mw[j];
+      *(uint32_t*)(v + i) = vw[j];
       if (copy) {
-        const u32x2 c = {adamw_bf16(pe[0]) | adamw_bf16(pe[1]) << 16, adamw_bf16(pe[2]) | adamw_bf16(pe[3]) << 16};
-        *(u32x2*)(copy + i) = c;
+        const u32x2 w = {adamw_bf16(pe[0]) | adamw_bf16(pe[1]) << 16, adamw_bf16(pe[2]) | adamw_bf16(pe[3]) << 16};
+        *(u32x2*)(copy + i) = w;
       }
-    } else {
+      if (lane == 0) {
+        m_exp[block] = (uint8_t)em[j];
+        v_exp[block] = (uint8_t)ev[j];
+      }
+    }
+    return;
+  }
+  for (int j = 0; j < 4; ++j) {
+    const int64_t block = block0 + 4 * j, i = block * kAdamwBlock + 4 * lane;
+    if (block * kAdamwBlock >= n) return;        // the whole wavefront
+    uint32_t em = m_exp[block], ev = v_exp[block], mc = 0, vc = 0;
+    float pe[4], ge[4];
 #pragma unroll
-      for (int q = 0; q < 4; ++q)
-        if (i + q < n) {
-          p[i + q] = pe[q];
-          m[i + q] = (uint8_t)(mc >> (8 * q));
-          v[i + q] = (uint8_t)(vc >> (8 * q));
-          if (copy) copy[i + q] = (uint16_t)adamw_bf16(pe[q]);
-        }
+    for (int q = 0; q < 4; ++q) {
+      const bool in = i + q < n;
+      pe[q] = in ? p[i + q] : 0.f;
+      ge[q] = in ? grad_at<BF16>(g, i + q) : 0.f;
+      mc |= (in ? (uint32_t)m[i + q] : 0u) << (8 * q);
+      vc |= (in ? (uint32_t)v[i + q] : 0u) << (8 * q);
+    }
+    adamw_8_block(c, (uint32_t)i, ge, pe, mc, vc, em, ev);
+#pragma unroll
+    for (int q = 0; q < 4; ++q)
+      if (i + q < n) {
+        p[i + q] = pe[q];
+        m[i + q] = (uint8_t)(mc >> (8 * q));
+        v[i + q] = (uint8_t)(vc >> (8 * q));
+        if (copy) copy[i + q] = (uint16_t)adamw_bf16(pe[q]);
+      }
+    if (lane == 0) {
+      m_exp[block] = (uint8_t)em;
+      v_exp[block] = (uint8_t)ev;
     }
   }
 }

@@ -62,12 +62,6 @@ struct Packed<bf16_t, 1> {
   static __device__ void store(bf16_t* p, const float (&v)[1]) { *p = norm_to_bits(v[0]); }
 };
 
-__device__ __forceinline__ float wave_sum(float x) {
-#pragma unroll
-  for (int m = 32; m > 0; m >>= 1) x += __shfl_xor(x, m);
-  return x;
-}
-
 // Sum over the W wavefronts of a row.  red: one float per wavefront, another array for every sum in flight: a wavefront that
 // writes one again has passed the barrier of the sum in between, behind which every wavefront had read it.
 template <int W>

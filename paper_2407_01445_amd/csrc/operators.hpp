@@ -1,5 +1,7 @@
 // Internal declarations of the operators in front of the loss: layer norm, linear layers, AdamW (not part of the ABI).
 #pragma once
+#include <type_traits>
+
 #include "fc_internal.hpp"
 
 namespace fc {
@@ -88,5 +90,29 @@ struct AdamwArgs {
 void launch_adamw_32(const AdamwArgs& a, hipStream_t s);
 void launch_adamw_8(const AdamwArgs& a, hipStream_t s);
 void launch_adamw_values(int moment, const uint8_t* codes, const uint8_t* exps, int64_t n, float* out, hipStream_t s);
+
+// ---- sums and maxima over a wavefront -------------------------------------------------------------------------------------
+// Inside rows of 16 lanes by lane permutes of the vector unit, over the four rows by scalar reads: no trip through LDS, which takes
+// ten times as long, and a result that is known to be the same in every lane.
+template <typename T, typename Op>
+__device__ __forceinline__ T wave_reduce(T x, Op&& op) {
+#ifdef __AMDGCN__
+  static_assert(sizeof(T) == 4, "one register");
+  auto moved = [](T v, auto control) {
+    return __builtin_bit_cast(T, __builtin_amdgcn_update_dpp(0, __builtin_bit_cast(int, v), decltype(control)::value, 0xf, 0xf, true));
+  };
+  x = op(x, moved(x, std::integral_constant<int, 0xB1>{}));       // lanes 1 0 3 2 of four
+  x = op(x, moved(x, std::integral_constant<int, 0x4E>{}));       // lanes 2 3 0 1
+  x = op(x, moved(x, std::integral_constant<int, 0x141>{}));      // mirrored in eight
+  x = op(x, moved(x, std::integral_constant<int, 0x140>{}));      // mirrored in sixteen
+  auto row = [&](int lane) { return __builtin_bit_cast(T, __builtin_amdgcn_readlane(__builtin_bit_cast(int, x), lane)); };
+  return op(op(row(0), row(16)), op(row(32), row(48)));
+#else
+  for (int m = 1; m < 64; m *= 2) x = op(x, __shfl_xor(x, m));
+  return x;
+#endif
+}
+__device__ __forceinline__ float wave_sum(float x) { return wave_reduce(x, [](float a, float b) { return a + b; }); }
+__device__ __forceinline__ uint32_t wave_largest(uint32_t x) { return wave_reduce(x, [](uint32_t a, uint32_t b) { return a > b ? a : b; }); }
 
 }  // namespace fc

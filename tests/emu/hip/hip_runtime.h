@@ -90,6 +90,7 @@ extern dim3 blockDim, gridDim;
 #define __builtin_amdgcn_wave_barrier() emu::t_wave->bar.wait()
 #define __builtin_amdgcn_exp2f(x) exp2f(x)
 #define __builtin_amdgcn_rcpf(x) (1.0f / (x))
+#define __builtin_amdgcn_sqrtf(x) sqrtf(x)
 #define __fmul_rn(a, b) ((a) * (b))
 static inline float __uint_as_float(uint32_t u) { float f; memcpy(&f, &u, 4); return f; }
 static inline uint32_t __float_as_uint(float f) { uint32_t u; memcpy(&u, &f, 4); return u; }
