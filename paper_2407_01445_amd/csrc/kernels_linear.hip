@@ -69,7 +69,7 @@ struct Operand {
   }
   // requests the 64 of k from k0 on into the panel at lds; what lies at or beyond `end` comes as zeros
   __device__ __forceinline__ void request(int64_t k0, int64_t end, uint32_t lds) const {
-    const bf16_t* at = base + (BY_DEPTH ? k0 * ld : k0);
+    const bf16_t* at = wave_uniform(base + (BY_DEPTH ? k0 * ld : k0));
     const uint32_t to = lds + (uint32_t)(wave * kLoads) * 1024u;
     if (k0 + kDepth <= end) {
 #pragma unroll
@@ -142,6 +142,11 @@ __device__ __forceinline__ void Tile<PD, QD, NI, NJ, WN, WM, S>::run(const Linea
     p.request(k0 + (int64_t)stage * kDepth, end, slot);
     q.request(k0 + (int64_t)stage * kDepth, end, slot + (uint32_t)OpP::kBytes);
   };
+  float my_bias = 0.f;
+  if (a.bias && lane < 32 * NI) {
+    const int64_t n = n0 + wn * NI * 32 + lane;
+    my_bias = a.bias[n < a.N ? n : a.N - 1];
+  }
   f32x16 acc[NI][NJ];
 #pragma unroll
   for (int i = 0; i < NI; ++i)
@@ -223,20 +228,14 @@ __device__ __forceinline__ void Tile<PD, QD, NI, NJ, WN, WM, S>::run(const Linea
     for (int e = 0; e < 8; ++e) v[e] = acc[h >> 1][j][8 * (h & 1) + e];
     exchange_halves(v);
   };
-  auto m_of = [&](int j) { return m0 + (wm * NJ + j) * 32 + lr; };
-  auto n_of = [&](int h) { return n0 + wn * NI * 32 + 16 * h + 8 * hk; };
-  if (splits > 1) {
-#pragma unroll
-    for (int j = 0; j < NJ; ++j)
-#pragma unroll
-      for (int h = 0; h < 2 * NI; ++h) {
-        float v[8];
-        values(j, h, v);
-        if (m_of(j) < a.M && n_of(h) < a.N) store_f32<8>(a.partial + ((int64_t)split * a.M + m_of(j)) * a.N + n_of(h), v);
-      }
-  } else {
-    finish_tile<!PD, NJ, 2 * NI>(a, values, m_of, n_of);
-  }
+  FC_FENCE();
+  __builtin_amdgcn_s_barrier();                // the ring is read for the last time: its room is the epilogue's
+  FC_FENCE();
+  static_assert(WAVES * kFinishRoom<NI> <= kRing, "every wavefront has its room");
+  char* room = ring + wave * kFinishRoom<NI>;
+  const int64_t m_wave = m0 + wm * NJ * 32, n_wave = n0 + wn * NI * 32;
+  if (splits > 1) keep_partial<NJ, NI>(a.partial + (int64_t)split * a.M * a.N, a.M, a.N, room, m_wave, n_wave, lane, values);
+  else finish_tile<PD ? kWeightGradient : (QD ? kInputGradient : kForward), NJ, NI>(a, room, m_wave, n_wave, lane, my_bias, values);
 }
 
 template <bool PD, bool QD, int NI, int NJ, int WN, int WM, int S>

@@ -138,85 +138,170 @@ __device__ __forceinline__ void finish_values(const LinearArgs& a, float (&z)[V]
 
 // ---- the epilogue of a wavefront's part of a tile --------------------------------------------------------------------------
 //
-// Eight neighbouring values of an output row at a time, groups h = 0 .. G - 1 side by side in a row of blocks.  Vector memory
-// operations complete in the order of their issue, stores too: a load behind stores waits for them.  So everything that the
-// epilogue reads is requested ahead of the stores: the bias before the first, residual and pre three groups
-// ahead.
-struct Held8 { u32x4 lo, hi; };                 // eight bf16 (lo) or fp32 values as they lie in memory
-__device__ __forceinline__ void hold(Held8& x, const void* p, int64_t at, bool bf16) {
-  if (bf16) {
-    x.lo = *(const u32x4*)((const bf16_t*)p + at);
+// A lane holds eight neighbouring values of a row, 32 lanes 32 rows: stored as they are, an instruction writes 32 bytes of each of
+// 32 lines, which costs the memory system several times what whole lines do (16384 x 4096 twice in bf16: 184 us a call, and 370
+// where the L2 does not gather the pieces).  So 32 rows at a time pass through LDS that is this wavefront's own, in pieces of 16
+// bytes at piece ^ (row mod pieces), and leave, or come, as whole stretches of a row.
+//
+// Vector memory operations complete in the order of their issue, stores too: a load behind stores waits for them.  So everything
+// that the epilogue reads is requested ahead of the stores: the bias before the first, residual and pre of 32 rows before the
+// stores of the 32 in front.
+template <int PIECES>
+__device__ __forceinline__ int piece_at(int row, int piece) { return (row * PIECES + (piece ^ (row & (PIECES - 1)))) * 16; }
+
+// 32 rows of PIECES times 16 bytes between memory and registers: lane l has piece l mod PIECES of rows l / PIECES + ...
+template <int PIECES>
+struct RowsInFlight {
+  static constexpr int kParts = PIECES / 2;          // 32 PIECES / 64
+  u32x4 part[kParts];
+  static __device__ __forceinline__ int row(int i, int lane) { return i * (64 / PIECES) + lane / PIECES; }
+  // from rows m .. of a matrix of elements of `size` bytes, columns n ..; rows and columns that do not exist repeat others
+  __device__ __forceinline__ void load(const void* p, int64_t ld, int64_t m, int64_t n, int64_t M, int64_t N, int size, int lane) {
+    int64_t c = n + (lane % PIECES) * (16 / size);
+    c = c < N ? c : N - 8;
+#pragma unroll
+    for (int i = 0; i < kParts; ++i) {
+      const int64_t r = m + row(i, lane) < M ? m + row(i, lane) : M - 1;
+      part[i] = *(const u32x4*)((const char*)p + (r * ld + c) * size);
+    }
+  }
+  // from LDS to memory, at most four pieces in registers
+  static __device__ __forceinline__ void store(const char* room, void* p, int64_t ld, int64_t m, int64_t n, int64_t M, int64_t N,
+                                               int size, bool stream, int lane) {
+    const int64_t c = n + (lane % PIECES) * (16 / size);
+    char* to = (char*)p + ((m + lane / PIECES) * ld + c) * size;
+    const int64_t step = (64 / PIECES) * ld * size;
+#pragma unroll
+    for (int i = 0; i < kParts; ++i, to += step) {
+      const u32x4 w = *(const u32x4*)(room + piece_at<PIECES>(row(i, lane), lane % PIECES));
+      if (m + row(i, lane) < M && c < N) {
+        if (stream) __builtin_nontemporal_store(w, (u32x4*)to);
+        else *(u32x4*)to = w;
+      }
+      if (i % 4 == 3) FC_PIN();
+    }
+  }
+  __device__ __forceinline__ void to_lds(char* room, int lane) const {
+#pragma unroll
+    for (int i = 0; i < kParts; ++i) *(u32x4*)(room + piece_at<PIECES>(row(i, lane), lane % PIECES)) = part[i];
+  }
+};
+// eight values of a row, columns 8 chunk ..
+template <bool BF16, int CHUNKS>
+__device__ __forceinline__ void put_values(char* room, int row, int chunk, const float (&v)[8]) {
+  if constexpr (BF16) {
+    store_bf16<8>((bf16_t*)(room + piece_at<CHUNKS>(row, chunk)), v);
   } else {
-    x.lo = *(const u32x4*)((const float*)p + at);
-    x.hi = *(const u32x4*)((const float*)p + at + 4);
+    *(float4*)(room + piece_at<2 * CHUNKS>(row, 2 * chunk)) = make_float4(v[0], v[1], v[2], v[3]);
+    *(float4*)(room + piece_at<2 * CHUNKS>(row, 2 * chunk + 1)) = make_float4(v[4], v[5], v[6], v[7]);
   }
 }
-__device__ __forceinline__ float held_value(const Held8& x, int i, bool bf16) {
-  const float wide = __uint_as_float(i < 4 ? x.lo[i & 3] : x.hi[i & 3]);
-  const uint32_t w = x.lo[i >> 1];
-  return bf16 ? __uint_as_float(i & 1 ? w & 0xffff0000u : w << 16) : wide;
-}
-// values(j, h, v): the eight sums of group h of row of blocks j, this lane's; its output row is m_of(j), its first column n_of(h).
-template <int ACT, int ROWS, int G, typename Values, typename MOf, typename NOf>
-__device__ __forceinline__ void finish_tile_act(const LinearArgs& a, Values&& values, MOf&& m_of, NOf&& n_of) {
-  const bool slope = ACT != FASTCLIP_ACT_NONE && a.pre_in, out_bf16 = a.out_bf16;
-  float bias[G][8];
-#pragma unroll
-  for (int h = 0; h < G; ++h) {
-#pragma unroll
-    for (int e = 0; e < 8; ++e) bias[h][e] = 0.f;
-    if (a.bias) load_f32<8>(bias[h], a.bias + (n_of(h) < a.N ? n_of(h) : a.N - 8));
+template <bool BF16, int CHUNKS>
+__device__ __forceinline__ void get_values(const char* room, int row, int chunk, float (&v)[8]) {
+  if constexpr (BF16) {
+    load_bf16<8>(v, (const bf16_t*)(room + piece_at<CHUNKS>(row, chunk)));
+  } else {
+    const float4 a = *(const float4*)(room + piece_at<2 * CHUNKS>(row, 2 * chunk));
+    const float4 b = *(const float4*)(room + piece_at<2 * CHUNKS>(row, 2 * chunk + 1));
+    v[0] = a.x; v[1] = a.y; v[2] = a.z; v[3] = a.w;
+    v[4] = b.x; v[5] = b.y; v[6] = b.z; v[7] = b.w;
   }
-  constexpr int kAhead = 3;                      // groups
-  Held8 extra[kAhead + 1];                       // pre_in or residual: a call has at most one of the two
-  auto request = [&](int t) {
-    const int64_t m = m_of(t / G) < a.M ? m_of(t / G) : a.M - 1, n = n_of(t % G) < a.N ? n_of(t % G) : a.N - 8;
-    if (slope) hold(extra[t % (kAhead + 1)], a.pre_in, m * a.ld_pre + n, true);
-    else if (a.residual) hold(extra[t % (kAhead + 1)], a.residual, m * a.ld_res + n, out_bf16);
+}
+// a wavefront's LDS for NI blocks of 32 columns: 32 rows of the output in fp32, and of pre in bf16; the bias
+template <int NI>
+constexpr int kFinishRoom = 32 * 32 * NI * 6 + 32 * NI * 4;
+
+enum LinearPass { kForward, kInputGradient, kWeightGradient };
+// my_bias: of column n0 + lane (the first 32 NI lanes); values(j, h, v): the eight sums of columns n0 + 16 h + 8 (lane / 32) .. of
+// row m0 + 32 j + lane mod 32.
+template <LinearPass PASS, int ACT, bool OUT_BF16, int ROWS, int NI, typename Values>
+__device__ __forceinline__ void finish_tile_act(const LinearArgs& a, char* room, int64_t m0, int64_t n0, int lane, float my_bias,
+                                                Values&& values) {
+  constexpr int G = 2 * NI, CHUNKS = 4 * NI, kOut = OUT_BF16 ? CHUNKS : 2 * CHUNKS, kSize = OUT_BF16 ? 2 : 4;
+  constexpr bool kSlope = PASS == kInputGradient && ACT != FASTCLIP_ACT_NONE;
+  const int lr = lane & 31, hk = lane >> 5;
+  char* pre_room = room + 32 * 32 * NI * 4;
+  float* bias = (float*)(room + 32 * 32 * NI * 6);
+  if (PASS == kForward && a.bias && lane < 32 * NI) bias[lane] = my_bias;
+  const bool residual = PASS == kForward && a.residual, keep = PASS == kForward && a.pre_out;
+  RowsInFlight<kSlope ? CHUNKS : kOut> rows;             // pre or residual
+  auto request = [&](int j) {
+    if constexpr (kSlope) rows.load(a.pre_in, a.ld_pre, m0 + 32 * j, n0, a.M, a.N, 2, lane);
+    else if (residual) rows.load(a.residual, a.ld_res, m0 + 32 * j, n0, a.M, a.N, kSize, lane);
   };
-#pragma unroll
-  for (int t = 0; t < kAhead && t < ROWS * G; ++t) request(t);
+  request(0);
 #pragma unroll
   for (int j = 0; j < ROWS; ++j) {
-    const int64_t m = m_of(j);
-    char* out = (char*)a.out + (m * a.ld_out) * (out_bf16 ? 2 : 4);
-    bf16_t* pre = (bf16_t*)a.pre_out + m * a.ld_pre;
+    if constexpr (kSlope) rows.to_lds(pre_room, lane);
+    else if (residual) rows.to_lds(room, lane);
+    if (j + 1 < ROWS) request(j + 1);
+    __builtin_amdgcn_wave_barrier();
+    float z[2][8];                                       // pre of this group and of the next
+    if constexpr (kSlope) get_values<true, CHUNKS>(pre_room, lr, hk, z[0]);
 #pragma unroll
     for (int h = 0; h < G; ++h) {
-      const int t = j * G + h;
-      if (t + kAhead < ROWS * G) request(t + kAhead);
-      const Held8& with = extra[t % (kAhead + 1)];
-      const int64_t n = n_of(h);
       float v[8];
+      if constexpr (kSlope) {
+        if (h + 1 < G) get_values<true, CHUNKS>(pre_room, lr, 2 * (h + 1) + hk, z[(h + 1) & 1]);
+      }
       values(j, h, v);
+      if (PASS == kForward && a.bias) {
+        const float4 lo = *(const float4*)(bias + 16 * h + 8 * hk), hi = *(const float4*)(bias + 16 * h + 8 * hk + 4);
+        v[0] += lo.x; v[1] += lo.y; v[2] += lo.z; v[3] += lo.w;
+        v[4] += hi.x; v[5] += hi.y; v[6] += hi.z; v[7] += hi.w;
+      }
+      if (keep) put_values<true, CHUNKS>(pre_room, lr, 2 * h + hk, v);
+      if constexpr (kSlope) {
 #pragma unroll
-      for (int e = 0; e < 8; ++e) v[e] += bias[h][e];
-      const bool in = m < a.M && n < a.N;
-      if (a.pre_out && in) store_bf16<8>(pre + n, v);
-      if (slope) {
-#pragma unroll
-        for (int e = 0; e < 8; ++e) v[e] *= activation_slope<ACT>(held_value(with, e, true));
-      } else if constexpr (ACT != FASTCLIP_ACT_NONE) {
+        for (int e = 0; e < 8; ++e) v[e] *= activation_slope<ACT>(z[h & 1][e]);
+      } else {
 #pragma unroll
         for (int e = 0; e < 8; ++e) v[e] = activate<ACT>(v[e]);
       }
-      if (a.residual) {
+      if (residual) {                                    // lies where the result goes
+        float t[8];
+        get_values<OUT_BF16, CHUNKS>(room, lr, 2 * h + hk, t);
 #pragma unroll
-        for (int e = 0; e < 8; ++e) v[e] += held_value(with, e, out_bf16);
+        for (int e = 0; e < 8; ++e) v[e] += t[e];
       }
-      if (in) {
-        if (out_bf16) store_bf16<8>((bf16_t*)out + n, v);
-        else store_f32<8>((float*)out + n, v);
-      }
+      put_values<OUT_BF16, CHUNKS>(room, lr, 2 * h + hk, v);
       FC_PIN();      // the sums of one group at a time in registers of their own
     }
+    __builtin_amdgcn_wave_barrier();
+    if (keep) RowsInFlight<CHUNKS>::store(pre_room, a.pre_out, a.ld_pre, m0 + 32 * j, n0, a.M, a.N, 2, a.stream_out, lane);
+    RowsInFlight<kOut>::store(room, a.out, a.ld_out, m0 + 32 * j, n0, a.M, a.N, kSize, a.stream_out, lane);
+    __builtin_amdgcn_wave_barrier();
   }
 }
-template <bool HAS_ACT, int ROWS, int G, typename Values, typename MOf, typename NOf>
-__device__ __forceinline__ void finish_tile(const LinearArgs& a, Values&& values, MOf&& m_of, NOf&& n_of) {
-  if (HAS_ACT && a.act == FASTCLIP_ACT_GELU) finish_tile_act<FASTCLIP_ACT_GELU, ROWS, G>(a, values, m_of, n_of);
-  else if (HAS_ACT && a.act == FASTCLIP_ACT_QUICK_GELU) finish_tile_act<FASTCLIP_ACT_QUICK_GELU, ROWS, G>(a, values, m_of, n_of);
-  else finish_tile_act<FASTCLIP_ACT_NONE, ROWS, G>(a, values, m_of, n_of);
+template <LinearPass PASS, int ROWS, int NI, typename Values>
+__device__ __forceinline__ void finish_tile(const LinearArgs& a, char* room, int64_t m0, int64_t n0, int lane, float my_bias,
+                                            Values&& values) {
+#define FC_FINISH(ACT)                                                                                    \
+  do {                                                                                                    \
+    if (a.out_bf16) finish_tile_act<PASS, ACT, true, ROWS, NI>(a, room, m0, n0, lane, my_bias, values);   \
+    else finish_tile_act<PASS, ACT, false, ROWS, NI>(a, room, m0, n0, lane, my_bias, values);             \
+  } while (0)
+  if (PASS != kWeightGradient && a.act == FASTCLIP_ACT_GELU) FC_FINISH(FASTCLIP_ACT_GELU);
+  else if (PASS != kWeightGradient && a.act == FASTCLIP_ACT_QUICK_GELU) FC_FINISH(FASTCLIP_ACT_QUICK_GELU);
+  else FC_FINISH(FASTCLIP_ACT_NONE);
+#undef FC_FINISH
+}
+// ... of a split: the sums themselves, fp32
+template <int ROWS, int NI, typename Values>
+__device__ __forceinline__ void keep_partial(float* to, int64_t M, int64_t N, char* room, int64_t m0, int64_t n0, int lane, Values&& values) {
+#pragma unroll
+  for (int j = 0; j < ROWS; ++j) {
+#pragma unroll
+    for (int h = 0; h < 2 * NI; ++h) {
+      float v[8];
+      values(j, h, v);
+      put_values<false, 4 * NI>(room, lane & 31, 2 * h + (lane >> 5), v);
+      FC_PIN();
+    }
+    __builtin_amdgcn_wave_barrier();
+    RowsInFlight<8 * NI>::store(room, to, N, m0 + 32 * j, n0, M, N, 4, false, lane);
+    __builtin_amdgcn_wave_barrier();
+  }
 }
 
 // Which output tile and split a workgroup takes.  Workgroups go to the eight XCDs in turn, each with an L2 of its own: those of

@@ -43,6 +43,7 @@ struct LinearArgs {
   const void* pre_in;      // gradient of the input: [M, ld_pre] or nullptr
   int64_t ld_pre;
   int act;                 // fastclip_activation: of z, or of which the derivative is taken with pre_in
+  bool stream_out;         // the outputs are larger than the caches: stored past them
   float* dbias;            // gradient of the weight: [M], sums of P over k, or nullptr
   float* partial;          // workspace: [splits][M][N] and behind them [bias_parts][M] for dbias
 };

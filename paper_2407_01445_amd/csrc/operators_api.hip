@@ -91,6 +91,9 @@ static fastclip_status run_linear(LinearArgs& a, void* workspace, size_t workspa
     if (workspace_bytes < plan.bytes) return FASTCLIP_ERR_WORKSPACE;
     a.partial = (float*)workspace;
   }
+  // Outputs that the L2s (32 MiB) could not hold for the next kernel are stored past them and leave them to the operands: 16384 x
+  // 4096 in bf16 and as much of pre 174 us -> 167; half of it is no slower either way.
+  a.stream_out = a.M * a.N * ((a.out_bf16 ? 2 : 4) + (a.pre_out ? 2 : 0)) > ((int64_t)64 << 20);
   if (a.bf16) launch_linear_bf16(a, plan, s);
   else launch_linear_f32(a, plan, s);
   if (plan.splits > 1) launch_linear_join(a, plan, s);
