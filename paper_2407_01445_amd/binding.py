@@ -519,17 +519,28 @@ def make_adamw_tensor(*, param, grad, m, v, param_bf16=None, weight_decay=0.0, m
     """Contiguous CUDA tensors of one size: param fp32, grad fp32 or bf16, m and v fp32 or uint8 (then with the blocks'
     exponents).  The struct keeps them referenced."""
     n = param.numel()
+    blocks = -(-n // ADAMW_BLOCK)
     parts = (param, grad, m, v, param_bf16, m_exp, v_exp)
-    for i, t in enumerate(parts):
+    addresses, types = [], []
+    for t, want in zip(parts, (n, n, n, n, n, blocks, blocks)):
         if t is None:
+            addresses.append(None)
+            types.append(None)
             continue
         if not t.is_contiguous():
             raise ValueError("adamw tensors must be contiguous")
-        if t.numel() != (n if i < 5 else -(-n // ADAMW_BLOCK)):
-            raise ValueError("param, grad, m, v and param_bf16 must have the same number of elements" if i < 5 else
-                             "an exponent for every block of %d elements" % ADAMW_BLOCK)
-    out = fastclip_adamw_tensor(*map(_ptr, parts), n, weight_decay, 0)
-    out._keepalive, out._types = parts, tuple(None if t is None else t.dtype for t in parts)
+        if t.numel() != want:
+            raise ValueError("param, grad, m, v and param_bf16 must have the same number of elements, the exponents one for every "
+                             "block of %d" % ADAMW_BLOCK)
+        if not t.is_cuda:
+            types.append(TypeError)
+            continue
+        addresses.append(t.data_ptr())
+        types.append(t.dtype)
+    if TypeError in types:
+        raise TypeError("fastclip buffers must be device tensors")
+    out = fastclip_adamw_tensor(*addresses, n, weight_decay, 0)
+    out._keepalive, out._types = parts, tuple(types)
     return out
 
 

@@ -264,6 +264,158 @@ __global__ void __launch_bounds__(256, 2) k_linear_bands(LinearArgs a, uint32_t 
   }
 }
 
+// ---- few tiles: latency -----------------------------------------------------------------------------------------------------
+//
+// Where the tiles are few, what counts is how soon the last product of a tile is done.  A workgroup forms 32 x 32 of the output,
+// its four wavefronts take every fourth 64 of k, each with two stages of LDS of its own, and meet once, to add up: no barrier in
+// the depth.
+constexpr uint32_t kPanel = 32 * 128;            // bytes of 32 rows (columns) of a stage
+// 32 rows (columns) of an operand for one wavefront.  LDS image by rows as above; by depth 64 bytes a row of k, four of which are
+// a read.
+template <bool BY_DEPTH>
+struct Operand32b {
+  static constexpr int kLoads = 4;               // of 1 KiB
+  const bf16_t* base;
+  int64_t ld;
+  int lane;
+  uint32_t off[kLoads];
+  __device__ __forceinline__ int depth_of(int i) const {
+    if constexpr (BY_DEPTH) return 16 * i + (lane >> 2);
+    return 8 * ((lane & 7) ^ row_swizzle(8 * i + (lane >> 3)));
+  }
+  __device__ __forceinline__ void open(const bf16_t* matrix, int64_t ld_, int64_t first, int64_t count, int lane_) {
+    ld = ld_; lane = lane_;
+    base = matrix + (BY_DEPTH ? first : first * ld);
+    const int left = (int)(count - first < 32 ? count - first : 32);
+#pragma unroll
+    for (int i = 0; i < kLoads; ++i) {
+      if constexpr (BY_DEPTH) {
+        const int piece = 8 * (lane & 3) < left ? lane & 3 : left / 8 - 1;
+        off[i] = (uint32_t)depth_of(i) * (uint32_t)ld * 2u + (uint32_t)piece * 16u;
+      } else {
+        const int row = 8 * i + (lane >> 3) < left ? 8 * i + (lane >> 3) : left - 1;
+        off[i] = (uint32_t)row * (uint32_t)ld * 2u + (uint32_t)depth_of(i) * 2u;
+      }
+    }
+  }
+  __device__ __forceinline__ void request(int64_t k0, int64_t end, uint32_t lds) const {
+    const bf16_t* at = wave_uniform(base + (BY_DEPTH ? k0 * ld : k0));
+#pragma unroll
+    for (int i = 0; i < kLoads; ++i) {
+      if (k0 + kDepth <= end) dma16(at, off[i], lds + (uint32_t)i * 1024u);
+      else dma16_from(k0 + depth_of(i) < end ? (const char*)at + off[i] : (const char*)g_zero_words, lds + (uint32_t)i * 1024u);
+    }
+  }
+  __device__ __forceinline__ bf16x8 read(const char* panel, int s) const {
+    const int lr = lane & 31, h = lane >> 5;
+    if constexpr (BY_DEPTH) {
+      const int n = ((lane >> 4) & 1) * 16 + 4 * (lane & 3), k = 16 * s + 8 * h + ((lane & 15) >> 2);
+      u32x2 half[2];
+#pragma unroll
+      for (int j = 0; j < 2; ++j)
+        half[j] = __builtin_bit_cast(
+            u32x2, __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_v4s*)(uintptr_t)lds_addr(panel + (k + 4 * j) * 64 + n * 2)));
+      return join_halves(half[0], half[1]);
+    } else {
+      return *(const bf16x8*)(panel + lr * 128 + (((2 * s + h) ^ row_swizzle(lr)) << 4));
+    }
+  }
+};
+
+template <bool PD, bool QD>
+__global__ void __launch_bounds__(256) k_linear_few(LinearArgs a, uint32_t rows, uint32_t cols, int splits, int64_t slice) {
+  __shared__ __attribute__((aligned(1024))) char ring[4 * 4 * kPanel];       // per wavefront two stages; then the parts of the sums
+  const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
+  const TilePlace place = tile_place(blockIdx.x, gridDim.x, rows, cols);
+  const int64_t m0 = place.m * 32, n0 = place.n * 32, k0 = place.split * slice;
+  const int64_t end = k0 + slice < a.K ? k0 + slice : a.K;
+  Operand32b<PD> p;
+  Operand32b<QD> q;
+  p.open((const bf16_t*)a.p, a.ldp, m0, a.M, lane);
+  q.open((const bf16_t*)a.q, a.ldq, n0, a.N, lane);
+  f32x16 acc[2];
+#pragma unroll
+  for (int i = 0; i < 2; ++i)
+#pragma unroll
+    for (int v = 0; v < 16; ++v) acc[i][v] = 0.f;
+  const bool sums = PD && QD && a.dbias && place.n == 0;
+  float total = 0.f;
+  constexpr int64_t kStep = 4 * kDepth;
+  const char* mine = ring + wave * 4 * kPanel;
+  const uint32_t mine_at = lds_addr(mine);
+  auto request = [&](int64_t k, uint32_t at) {
+    p.request(k, end, mine_at + at);
+    q.request(k, end, mine_at + at + kPanel);
+  };
+  uint32_t here = 0;
+  if (k0 + wave * kDepth < end) request(k0 + wave * kDepth, 0);
+  for (int64_t k = k0 + wave * kDepth; k < end; k += kStep) {
+    if (k + kStep < end) {
+      request(k + kStep, here ^ (2 * kPanel));
+      FC_WAIT_VMCNT8();                          // the older stage's have landed
+    } else {
+      FC_WAIT_VMCNT0();
+    }
+    FC_FENCE();
+    __builtin_amdgcn_wave_barrier();
+    bf16x8 x[4], y[4];
+#pragma unroll
+    for (int s = 0; s < 4; ++s) {
+      x[s] = p.read(mine + here, s);
+      y[s] = q.read(mine + here + kPanel, s);
+    }
+#pragma unroll
+    for (int s = 0; s < 4; ++s) acc[s & 1] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(x[s], y[s], acc[s & 1], 0, 0, 0);
+    if constexpr (PD && QD) {
+      if (sums) {
+        const bf16x2 ones = __builtin_bit_cast(bf16x2, 0x3f803f80u);
+        float some[4] = {0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+        for (int s = 0; s < 4; ++s) {
+          const u32x4 w = __builtin_bit_cast(u32x4, x[s]);
+#pragma unroll
+          for (int e = 0; e < 4; ++e) {
+            const uint32_t pair = w[e];
+            some[e] = __builtin_amdgcn_fdot2_f32_bf16(__builtin_bit_cast(bf16x2, pair), ones, some[e], false);
+          }
+        }
+        total += (some[0] + some[1]) + (some[2] + some[3]);
+      }
+    }
+    FC_FENCE();                                  // the stage's reads are over before the next request takes its place
+    __builtin_amdgcn_wave_barrier();
+    here ^= 2 * kPanel;
+  }
+
+  __syncthreads();
+  float(*parts)[16][64] = (float(*)[16][64])ring;
+  if (sums) {
+    parts[wave][0][lane] = total + __shfl_xor(total, 32);
+    __syncthreads();
+    if (tid < 32 && m0 + tid < a.M) {
+      float* to = splits > 1 ? a.partial + (int64_t)splits * a.M * a.N + (int64_t)place.split * a.M : a.dbias;
+      to[m0 + tid] = (parts[0][0][tid] + parts[1][0][tid]) + (parts[2][0][tid] + parts[3][0][tid]);
+    }
+    __syncthreads();
+  }
+#pragma unroll
+  for (int v = 0; v < 16; ++v) parts[wave][v][lane] = acc[0][v] + acc[1][v];
+  __syncthreads();
+  // four neighbouring values of a row by every thread: row r is accumulator 4 (r / 8) + r mod 4 of the lanes from 32 (r / 4 mod 2) on
+  const int r = tid >> 3, c = (tid & 7) * 4, v = (r >> 3) * 4 + (r & 3), from = ((r >> 2) & 1) * 32 + c;
+  float z[4] = {0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+  for (int w = 0; w < 4; ++w) {
+    const float4 part = *(const float4*)&parts[w][v][from];
+    z[0] += part.x; z[1] += part.y; z[2] += part.z; z[3] += part.w;
+  }
+  const int64_t m = m0 + r, n = n0 + c;
+  if (m < a.M && n < a.N) {
+    if (splits > 1) store_f32<4>(a.partial + ((int64_t)place.split * a.M + m) * a.N + n, z);
+    else finish_values<true, 4>(a, z, m, n);
+  }
+}
+
 // ---- sums of splits -----------------------------------------------------------------------------------------------------
 // V neighbouring values of the output by G lanes, each with every G-th split; behind the workgroups of the output those of dbias,
 // 32 values by 8 threads.  With one lane a value the loads of 64 splits follow each other: 24 us for 128 x 128 values, of which
@@ -339,24 +491,26 @@ void launch_linear_empty(const LinearArgs& a, hipStream_t s) {
 }
 
 // ---- plan -----------------------------------------------------------------------------------------------------------------
-// Measured (one MI355X, us; a stage is 64 of k).  A stage of a 64 x 64 tile takes 0.33 where its workgroup has a compute unit to
-// itself, 0.46 and 0.6 where two and three share it; of 128 x 128 0.62 and, two on a compute unit, 0.96; of 192 x 128 0.8 and 1.23;
-// of 256 x 256, alone, 1.67; the small tiles a sixth more with both operands by depth.  A round of workgroups starts and ends in
-// 2, 3, 4.5 and 9, the large tile in 26 where the value before the activation is kept: the epilogue and the stores of two
-// workgroups on a compute unit pass beneath the other one's products, the large tile has nobody.  Splits: a launch and the
-// traffic of their partial sums.
+// Measured (one MI355X, us; a stage is 64 of k).  A stage of a 32 x 32 tile takes 0.08 where its workgroup has a compute unit to
+// itself and 0.1 where two share it; of 64 x 64 0.33, 0.46 and, three, 0.6; of 128 x 128 0.62 and, two, 0.96; of 192 x 128 0.8 and
+// 1.23; of 256 x 256, alone, 1.67; 64 x 64 and 128 x 128 a sixth more with both operands by depth.  A round of workgroups starts
+// and ends in 1.4, 2, 3, 4.5 and 9, the large tile in 14 where the value before the activation is kept.  Splits: a launch and the
+// traffic of their partial sums.  In fp32 a stage of 32 x 32 takes 0.36 and 0.64, of 64 x 64 1.4 and 2.3, their ends 1.7 and 3.
 static double rounds_of(int64_t n, double deep, int per_cu, const double (&stage)[3], double ends) {
   const int64_t places = 256 * per_cu, full = n / places, rest = n % places;
   double t = (double)full * (deep * stage[per_cu - 1] + ends);
   if (rest) t += deep * stage[rest <= 256 ? 0 : (rest <= 512 ? 1 : 2)] + ends;
   return t;
 }
-static const double kStage64[3] = {0.33, 0.46, 0.60}, kStage128[3] = {0.62, 0.96, 0.96}, kStage192[3] = {0.80, 1.23, 1.23},
-                    kStage256[3] = {1.67, 1.67, 1.67}, kStageF32[3] = {0.40, 0.48, 0.48};
+static const double kStage32[3] = {0.08, 0.10, 0.10}, kStage64[3] = {0.33, 0.46, 0.60}, kStage128[3] = {0.62, 0.96, 0.96},
+                    kStage192[3] = {0.80, 1.23, 1.23}, kStage256[3] = {1.67, 1.67, 1.67}, kStageF32[3] = {0.36, 0.64, 0.64},
+                    kStageF32_64[3] = {1.40, 2.30, 2.30};
 
-// What takes the least time by the figures above.  16384 rows of 1024 -> 4096 with GELU and pre kept: 256 x 256 222, bands of 192
-// rows 182; without either 146 and 149; 4096 -> 4096: 256 x 256 466, bands 494.  1024 rows of 1024 -> 1024: 64 x 64 9.5,
-// 128 x 128 13.5; 4096 rows: 19 and 15.  128 rows of 4096 -> 512: one split 25, eight 10.
+// What takes the least time by the figures above.  16384 rows of 1024 -> 4096 with quick GELU and pre kept: 256 x 256 170, bands of
+// 192 rows 167, 128 x 128 268; 4096 -> 4096: 256 x 256 466, bands 494.  1024 rows of 1024 -> 1024: 32 x 32 and 64 x 64 9.5,
+// 128 x 128 13.5; 4096 rows: 64 x 64 19, 128 x 128 15.  128 rows of 2048 -> 2048: 32 x 32 6.9, 64 x 64 14.6, four splits of it
+// 11.2; of 4096 -> 512: 32 x 32 10.5 and in two splits 9.6, 64 x 64 25.  fp32: 1000 rows of 760 -> 760: 32 x 32 19.8, 64 x 64
+// 23.7; 16000 of 600 -> 650: 165 and 153.
 LinearPlan plan_linear(int64_t M, int64_t N, int64_t K, bool bf16, bool by_depth, bool keeps, bool dbias) {
   static const int kSplits[] = {1, 2, 3, 4, 6, 8, 12, 16, 24, 32, 48, 64};
   auto count = [](int64_t x, int64_t t) { return (x + t - 1) / t; };
@@ -377,13 +531,15 @@ LinearPlan plan_linear(int64_t M, int64_t N, int64_t K, bool bf16, bool by_depth
       best.tile = tile; best.high = (int)high; best.low = (int)low; best.splits = s; best.slice = slice * kDepth;
     };
     if (!bf16) {
-      consider(32, 0, 0, rounds_of(count(M, 32) * count(N, 32) * s, deep, 2, kStageF32, 1.5));
+      consider(32, 0, 0, rounds_of(count(M, 32) * count(N, 32) * s, deep, 2, kStageF32, 1.7));
+      consider(64, 0, 0, rounds_of(n64 * s, deep, 2, kStageF32_64, 3.0));
       continue;
     }
+    if (n64 * s <= 512) consider(32, 0, 0, rounds_of(count(M, 32) * count(N, 32) * s, deep, 2, kStage32, 1.4));
     if (n64 <= 4096) consider(64, 0, 0, rounds_of(n64 * s, small_deep, 3, kStage64, 2.0));
     if (n64 <= 64) continue;
     consider(128, 0, count(M, 128), rounds_of(n128 * s, small_deep, 2, kStage128, 3.0));
-    if (n256 * s >= 64) consider(256, 0, 0, rounds_of(n256 * s, deep, 1, kStage256, keeps ? 26.0 : 9.0));
+    if (n256 * s >= 64) consider(256, 0, 0, rounds_of(n256 * s, deep, 1, kStage256, keeps ? 14.0 : 9.0));
     if (s > 1 || n128 <= 512 || by_depth) continue;
     // whole rounds of 192-row bands, or what leaves up to 24 bands of 128 rows for the last one
     for (int64_t low = 0; low <= 24 && low * 128 < M; ++low) {
@@ -397,8 +553,7 @@ LinearPlan plan_linear(int64_t M, int64_t N, int64_t K, bool bf16, bool by_depth
       consider(128, high, low, cost);
     }
   }
-  best.bias_parts = best.tile == 128 ? 2 * (int)cols : (best.tile == 256 ? 4 * (int)count(N, 256) : 2 * (int)count(N, 64));
-  if (!bf16) best.bias_parts = 1;
+  best.bias_parts = best.tile == 128 ? 2 * (int)cols : (best.tile == 256 ? 4 * (int)count(N, 256) : (best.tile == 64 ? 2 * (int)count(N, 64) : 1));
   best.bias_parts *= best.splits;
   if (best.splits > 1)
     best.bytes = round_up(sizeof(float) * ((size_t)best.splits * (size_t)(M * N) + (dbias ? (size_t)best.bias_parts * (size_t)M : 0)), 256);
@@ -415,7 +570,9 @@ static void launch_form(const LinearArgs& a, const LinearPlan& plan, hipStream_t
     return;
   }
   const uint32_t rows = (uint32_t)((a.M + plan.tile - 1) / plan.tile), cols = (uint32_t)((a.N + plan.tile - 1) / plan.tile);
-  if (plan.tile == 256)
+  if (plan.tile == 32)
+    hipLaunchKernelGGL((k_linear_few<PD, QD>), dim3(rows * cols * splits), dim3(256), 0, s, a, rows, cols, plan.splits, plan.slice);
+  else if (plan.tile == 256)
     hipLaunchKernelGGL((k_linear_bf16<PD, QD, 2, 4, 4, 2, 2>), dim3(rows * cols * splits), dim3(512), 0, s, a, rows, cols,
                        plan.splits, plan.slice);
   else

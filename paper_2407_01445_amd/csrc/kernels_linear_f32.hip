@@ -4,9 +4,10 @@
 //   out[m, n] = sum_k P[m, k] Q[n, k]
 //
 // The fp32 matrix cores take 64 cycles for the 128 operand words of a product, so that one wavefront needs little data at a time,
-// and wavefronts need not meet: four of them share a tile by taking every fourth block of 32 of k (a line of an operand by rows),
-// each with two blocks of LDS of its own, the next one on its way from memory by direct-to-LDS loads while the present one is
-// multiplied.  There is no barrier until they add up, each then finishing a quarter of the tile.  (Operands straight from memory
+// and wavefronts need not meet: each forms 32 x 32 of the output from LDS of its own, 32 of k (a line of an operand by rows) at a
+// time, the next block on its way from memory by direct-to-LDS loads while the present one is multiplied.  Where there are tiles
+// enough, a workgroup's four wavefronts have four of them, 64 x 64 in all, and no barrier; where there are few, they share one,
+// every fourth block of k each, and add up at the end, each finishing a quarter.  (Operands straight from memory
 // into registers instead, as the products want them, fetch 32 bytes of each of 32 lines per load and took twice as long.)  The
 // order of k inside a block is free as long as both operands keep to it: lanes below 32 take k = 8 s .. 8 s + 3, the others
 // 8 s + 4 .. 8 s + 7, which by rows is one 16-byte read for four products.  P gives the MFMA's rows, so that 32 lanes hold
@@ -41,7 +42,7 @@ typedef float Words32[4][4];       // [s][j]: k = 8 s + 4 h + j of a row (column
 template <bool BY_DEPTH, bool WIDE>
 struct Operand32 {
   static constexpr int kLoads = WIDE ? 4 : 16;     // wave loads of a block of k
-  const char* base;                // wave-uniform
+  const char* base;
   int64_t line;                    // bytes from one row (row of k) to the next
   uint32_t off[kLoads];            // this lane's bytes from there at depth 0
   int lane;
@@ -54,7 +55,7 @@ struct Operand32 {
   }
   __device__ __forceinline__ void open(const void* matrix, int64_t ld, int64_t first, int64_t count, int lane_) {
     line = ld * 4; lane = lane_;
-    base = wave_uniform((const char*)matrix + (BY_DEPTH ? first * 4 : first * line));
+    base = (const char*)matrix + (BY_DEPTH ? first * 4 : first * line);
     const int left = (int)(count - first < 32 ? count - first : 32);
 #pragma unroll
     for (int i = 0; i < kLoads; ++i) {
@@ -72,7 +73,7 @@ struct Operand32 {
   }
   // requests the block of k from k0 on (wave-uniform)
   __device__ __forceinline__ void request(int64_t k0, int64_t end, uint32_t lds) const {
-    const char* at = base + (BY_DEPTH ? k0 * line : k0 * 4);
+    const char* at = wave_uniform(base + (BY_DEPTH ? k0 * line : k0 * 4));
     constexpr uint32_t kStep = WIDE ? 1024 : 256;
     if (k0 + kBlock32 <= end) {
 #pragma unroll
@@ -103,7 +104,8 @@ struct Operand32 {
   }
 };
 
-template <bool PD, bool QD, bool WIDE>
+// SHARED: the four wavefronts share a tile.
+template <bool PD, bool QD, bool WIDE, bool SHARED>
 __global__ void __launch_bounds__(256) k_linear_f32(LinearArgs a, uint32_t rows, uint32_t cols, int splits, int64_t slice) {
   typedef Operand32<PD, WIDE> OpP;
   typedef Operand32<QD, WIDE> OpQ;
@@ -112,8 +114,9 @@ __global__ void __launch_bounds__(256) k_linear_f32(LinearArgs a, uint32_t rows,
   __shared__ __attribute__((aligned(1024))) char ring[4 * 2 * kBuffer];      // per wavefront two blocks; then the parts of the sums
   const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6), lr = lane & 31, hk = lane >> 5;
   const TilePlace place = tile_place(blockIdx.x, gridDim.x, rows, cols);
-  const int64_t m0 = place.m * 32, n0 = place.n * 32, k0 = place.split * slice;
-  const int64_t end = k0 + slice < a.K ? k0 + slice : a.K;
+  const int64_t m0 = SHARED ? place.m * 32 : place.m * 64 + 32 * (wave & 1), n0 = SHARED ? place.n * 32 : place.n * 64 + 32 * (wave >> 1);
+  if (!SHARED && (m0 >= a.M || n0 >= a.N)) return;
+  const int64_t k0 = place.split * slice, end = k0 + slice < a.K ? k0 + slice : a.K;
   OpP p;
   OpQ q;
   p.open(a.p, a.ldp, m0, a.M, lane);
@@ -123,10 +126,10 @@ __global__ void __launch_bounds__(256) k_linear_f32(LinearArgs a, uint32_t rows,
   for (int i = 0; i < 2; ++i)
 #pragma unroll
     for (int v = 0; v < 16; ++v) acc[i][v] = 0.f;
-  const bool sums = PD && QD && a.dbias && place.n == 0;      // this tile also sums P over the depth
+  const bool sums = PD && QD && a.dbias && n0 == 0;           // this tile also sums P over the depth
   float total = 0.f;
 
-  constexpr int64_t kStep = 4 * kBlock32;
+  constexpr int64_t kStep = (SHARED ? 4 : 1) * kBlock32;
   const char* mine = ring + wave * 2 * kBuffer;
   const uint32_t mine_at = lds_addr(mine);
   auto request = [&](int64_t k, uint32_t buffer) {
@@ -134,8 +137,9 @@ __global__ void __launch_bounds__(256) k_linear_f32(LinearArgs a, uint32_t rows,
     q.request(k, end, mine_at + buffer + kPanel32);
   };
   uint32_t here = 0;
-  if (k0 + wave * kBlock32 < end) request(k0 + wave * kBlock32, 0);
-  for (int64_t k = k0 + wave * kBlock32; k < end; k += kStep) {
+  const int64_t first = k0 + (SHARED ? wave * kBlock32 : 0);
+  if (first < end) request(first, 0);
+  for (int64_t k = first; k < end; k += kStep) {
     if (k + kStep < end) {
       request(k + kStep, here ^ kBuffer);
       wait_vmcnt<kRequests>();                   // the older block's have landed
@@ -164,29 +168,54 @@ __global__ void __launch_bounds__(256) k_linear_f32(LinearArgs a, uint32_t rows,
     here ^= kBuffer;
   }
 
-  __syncthreads();
-  float(*parts)[16][64] = (float(*)[16][64])ring;
-  if (sums) {
-    parts[wave][0][lane] = total + __shfl_xor(total, 32);
-    __syncthreads();
-    if (tid < 32 && m0 + tid < a.M) {
-      float* to = splits > 1 ? a.partial + (int64_t)splits * a.M * a.N + (int64_t)place.split * a.M : a.dbias;
-      to[m0 + tid] = (parts[0][0][tid] + parts[1][0][tid]) + (parts[2][0][tid] + parts[3][0][tid]);
+  float* bias_to = splits > 1 ? a.partial + (int64_t)splits * a.M * a.N + (int64_t)place.split * a.M : a.dbias;
+  const int64_t n = n0 + lr;
+  const bool in = n < a.N;
+  const float bias = a.bias && in ? a.bias[n] : 0.f;
+  if constexpr (!SHARED) {
+    if (sums) {
+      total += __shfl_xor(total, 32);
+      if (hk == 0 && m0 + lr < a.M) bias_to[m0 + lr] = total;
     }
+    auto row_of = [&](int v) { return m0 + 8 * (v >> 2) + 4 * hk + (v & 3); };
+    float extra[16];
+#pragma unroll
+    for (int v = 0; v < 16; ++v) extra[v] = splits == 1 && in && row_of(v) < a.M ? single_extra(a, row_of(v), n) : 0.f;
+#pragma unroll
+    for (int v = 0; v < 16; ++v) {
+      const int64_t m = row_of(v);
+      if (in && m < a.M) {
+        if (splits > 1) a.partial[((int64_t)place.split * a.M + m) * a.N + n] = acc[0][v] + acc[1][v];
+        else finish_single(a, acc[0][v] + acc[1][v], bias, extra[v], m, n);
+      }
+    }
+  } else {
     __syncthreads();
-  }
+    float(*parts)[16][64] = (float(*)[16][64])ring;
+    if (sums) {
+      parts[wave][0][lane] = total + __shfl_xor(total, 32);
+      __syncthreads();
+      if (tid < 32 && m0 + tid < a.M)
+        bias_to[m0 + tid] = (parts[0][0][tid] + parts[1][0][tid]) + (parts[2][0][tid] + parts[3][0][tid]);
+      __syncthreads();
+    }
 #pragma unroll
-  for (int v = 0; v < 16; ++v) parts[wave][v][lane] = acc[0][v] + acc[1][v];
-  __syncthreads();
-  // this wavefront finishes the accumulators number v with v mod 4 its own
+    for (int v = 0; v < 16; ++v) parts[wave][v][lane] = acc[0][v] + acc[1][v];
+    __syncthreads();
+    // this wavefront finishes the accumulators number v with v mod 4 its own
+    auto row_of = [&](int t) { return m0 + 8 * t + 4 * hk + wave; };
+    float extra[4];
 #pragma unroll
-  for (int t = 0; t < 4; ++t) {
-    const int v = 4 * t + wave;
-    const int64_t m = m0 + 8 * (v >> 2) + 4 * hk + (v & 3), n = n0 + lr;
-    float z[1] = {(parts[0][v][lane] + parts[1][v][lane]) + (parts[2][v][lane] + parts[3][v][lane])};
-    if (m < a.M && n < a.N) {
-      if (splits > 1) a.partial[((int64_t)place.split * a.M + m) * a.N + n] = z[0];
-      else finish_values<false, 1>(a, z, m, n);
+    for (int t = 0; t < 4; ++t) extra[t] = splits == 1 && in && row_of(t) < a.M ? single_extra(a, row_of(t), n) : 0.f;
+#pragma unroll
+    for (int t = 0; t < 4; ++t) {
+      const int v = 4 * t + wave;
+      const int64_t m = row_of(t);
+      const float z = (parts[0][v][lane] + parts[1][v][lane]) + (parts[2][v][lane] + parts[3][v][lane]);
+      if (in && m < a.M) {
+        if (splits > 1) a.partial[((int64_t)place.split * a.M + m) * a.N + n] = z;
+        else finish_single(a, z, bias, extra[t], m, n);
+      }
     }
   }
 }
@@ -196,11 +225,19 @@ static bool wide_f32(const void* p, int64_t ld, int64_t width) { return !((uintp
 
 template <bool PD, bool QD>
 static void launch_form_f32(const LinearArgs& a, const LinearPlan& plan, hipStream_t s) {
-  const uint32_t rows = (uint32_t)((a.M + 31) / 32), cols = (uint32_t)((a.N + 31) / 32);
+  const uint32_t rows = (uint32_t)((a.M + plan.tile - 1) / plan.tile), cols = (uint32_t)((a.N + plan.tile - 1) / plan.tile);
   const dim3 grid(rows * cols * (uint32_t)plan.splits);
   const bool wide = wide_f32(a.p, a.ldp, PD ? a.M : a.K) && wide_f32(a.q, a.ldq, QD ? a.N : a.K);
-  if (wide) hipLaunchKernelGGL((k_linear_f32<PD, QD, true>), grid, dim3(256), 0, s, a, rows, cols, plan.splits, plan.slice);
-  else hipLaunchKernelGGL((k_linear_f32<PD, QD, false>), grid, dim3(256), 0, s, a, rows, cols, plan.splits, plan.slice);
+#define FC_F32(WIDE, SHARED) \
+  hipLaunchKernelGGL((k_linear_f32<PD, QD, WIDE, SHARED>), grid, dim3(256), 0, s, a, rows, cols, plan.splits, plan.slice)
+  if (plan.tile == 32) {
+    if (wide) FC_F32(true, true);
+    else FC_F32(false, true);
+  } else {
+    if (wide) FC_F32(true, false);
+    else FC_F32(false, false);
+  }
+#undef FC_F32
 }
 
 void launch_linear_f32(const LinearArgs& a, const LinearPlan& plan, hipStream_t s) {

@@ -58,6 +58,10 @@ __device__ __forceinline__ void load_bf16(float (&x)[V], const bf16_t* p) {
     const u32x4 w = *(const u32x4*)p;
 #pragma unroll
     for (int i = 0; i < 8; ++i) x[i] = __uint_as_float(i & 1 ? w[i >> 1] & 0xffff0000u : w[i >> 1] << 16);
+  } else if constexpr (V == 4) {
+    const u32x2 w = *(const u32x2*)p;
+#pragma unroll
+    for (int i = 0; i < 4; ++i) x[i] = __uint_as_float(i & 1 ? w[i >> 1] & 0xffff0000u : w[i >> 1] << 16);
   } else {
 #pragma unroll
     for (int i = 0; i < V; ++i) x[i] = bf2f(p[i]);
@@ -68,6 +72,9 @@ __device__ __forceinline__ void store_bf16(bf16_t* p, const float (&x)[V]) {
   if constexpr (V == 8) {
     const u32x4 w = {pack_bf16x2(x[0], x[1]), pack_bf16x2(x[2], x[3]), pack_bf16x2(x[4], x[5]), pack_bf16x2(x[6], x[7])};
     *(u32x4*)p = w;
+  } else if constexpr (V == 4) {
+    const u32x2 w = {pack_bf16x2(x[0], x[1]), pack_bf16x2(x[2], x[3])};
+    *(u32x2*)p = w;
   } else {
 #pragma unroll
     for (int i = 0; i < V; ++i) p[i] = f2bf(x[i]);
@@ -79,6 +86,10 @@ __device__ __forceinline__ void load_f32(float (&x)[V], const float* p) {
     const f32x4_any a = *(const f32x4_any*)p, b = *(const f32x4_any*)(p + 4);
 #pragma unroll
     for (int i = 0; i < 8; ++i) x[i] = i < 4 ? a[i & 3] : b[i & 3];
+  } else if constexpr (V == 4) {
+    const f32x4_any a = *(const f32x4_any*)p;
+#pragma unroll
+    for (int i = 0; i < 4; ++i) x[i] = a[i];
   } else {
 #pragma unroll
     for (int i = 0; i < V; ++i) x[i] = p[i];
@@ -89,6 +100,8 @@ __device__ __forceinline__ void store_f32(float* p, const float (&x)[V]) {
   if constexpr (V == 8) {
     *(f32x4_any*)p = f32x4_any{x[0], x[1], x[2], x[3]};
     *(f32x4_any*)(p + 4) = f32x4_any{x[4], x[5], x[6], x[7]};
+  } else if constexpr (V == 4) {
+    *(f32x4_any*)p = f32x4_any{x[0], x[1], x[2], x[3]};
   } else {
 #pragma unroll
     for (int i = 0; i < V; ++i) p[i] = x[i];
@@ -134,6 +147,28 @@ __device__ __forceinline__ void finish_values(const LinearArgs& a, float (&z)[V]
   if (a.act == FASTCLIP_ACT_GELU) finish_values_act<BF16, FASTCLIP_ACT_GELU, V>(a, z, m, n);
   else if (a.act == FASTCLIP_ACT_QUICK_GELU) finish_values_act<BF16, FASTCLIP_ACT_QUICK_GELU, V>(a, z, m, n);
   else finish_values_act<BF16, FASTCLIP_ACT_NONE, V>(a, z, m, n);
+}
+
+// The same for single values of fp32 operands, with what a value needs of residual or pre fetched by the caller ahead of the
+// stores (single_extra).
+__device__ __forceinline__ float single_extra(const LinearArgs& a, int64_t m, int64_t n) {
+  if (a.pre_in) return ((const float*)a.pre_in)[m * a.ld_pre + n];
+  if (a.residual) return a.out_bf16 ? bf2f(((const bf16_t*)a.residual)[m * a.ld_res + n]) : ((const float*)a.residual)[m * a.ld_res + n];
+  return 0.f;
+}
+__device__ __forceinline__ void finish_single(const LinearArgs& a, float z, float bias, float extra, int64_t m, int64_t n) {
+  z += bias;
+  if (a.pre_out) ((float*)a.pre_out)[m * a.ld_pre + n] = z;
+  if (a.pre_in) {
+    if (a.act == FASTCLIP_ACT_GELU) z *= activation_slope<FASTCLIP_ACT_GELU>(extra);
+    else z *= activation_slope<FASTCLIP_ACT_QUICK_GELU>(extra);
+  } else {
+    if (a.act == FASTCLIP_ACT_GELU) z = activate<FASTCLIP_ACT_GELU>(z);
+    else if (a.act == FASTCLIP_ACT_QUICK_GELU) z = activate<FASTCLIP_ACT_QUICK_GELU>(z);
+    if (a.residual) z += extra;
+  }
+  if (a.out_bf16) ((bf16_t*)a.out)[m * a.ld_out + n] = f2bf(z);
+  else ((float*)a.out)[m * a.ld_out + n] = z;
 }
 
 // ---- the epilogue of a wavefront's part of a tile --------------------------------------------------------------------------

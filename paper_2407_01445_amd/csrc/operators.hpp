@@ -48,7 +48,7 @@ struct LinearArgs {
   float* partial;          // workspace: [splits][M][N] and behind them [bias_parts][M] for dbias
 };
 struct LinearPlan {
-  int tile;                // 32 (fp32), 64, 256: rows and columns of a workgroup's output tile; 128: bands of
+  int tile;                // 32, 64, 256: rows and columns of a workgroup's output tile; 128: bands of
   int high, low;           // ... 192 and then of 128 rows, 128 columns
   int splits;              // workgroups over the depth of a tile
   int64_t slice;           // depth of a split

@@ -83,7 +83,7 @@ int main(int argc, char** argv) {
       const bool bf16 = i % 4 != 0;
       const int64_t M = next(40000, 1), N = next(9000, bf16 ? 8 : 1), K = next(20000, 1);
       const fc::LinearPlan p = fc::plan_linear(M, N, K, bf16, i % 3 == 0, i % 3 == 1, i % 3 == 0);
-      const bool tiles = p.tile == 64 || (!bf16 && p.tile == 32) || (bf16 && p.tile == 256) ||
+      const bool tiles = p.tile == 64 || p.tile == 32 || (bf16 && p.tile == 256) ||
                          (bf16 && p.tile == 128 && p.high >= 0 && p.low >= 0 && p.high * 192 + p.low * 128 >= M &&
                           (p.low ? p.high * 192 + (p.low - 1) * 128 < M : (p.high - 1) * 192 < M) && !(i % 3 == 0 && p.high));
       const bool depth = p.splits >= 1 && p.slice % 64 == 0 && p.splits * p.slice >= K && (p.splits - 1) * p.slice < K;

@@ -412,7 +412,7 @@ def test_linear_sources_on_the_host(emu, tmp_path, rows, d_in, d_out, type, out_
 @pytest.mark.parametrize("type", ["bf16", "f32"])
 def test_linear_weight_gradient_over_split_rows_and_no_rows(emu, tmp_path, type):
     rng = np.random.default_rng(8)
-    rows, d_in, d_out = 1100, 24, 16
+    rows, d_in, d_out = (8200 if type == "bf16" else 1100), 24, 16      # deep enough for more than one split
     x, _, dy = matrices(rng, rows, d_in, d_out, type)
     numbers = [KIND[type], fc.F32, 0, rows, d_in, d_out, d_in, d_in, d_out, d_out, d_out]
     cfg = fc.make_linear_config(rows=rows, d_in=d_in, d_out=d_out, dtype=KIND[type], out_dtype=fc.F32)
