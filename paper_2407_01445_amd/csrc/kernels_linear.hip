@@ -300,10 +300,13 @@ struct Operand32b {
   }
   __device__ __forceinline__ void request(int64_t k0, int64_t end, uint32_t lds) const {
     const bf16_t* at = wave_uniform(base + (BY_DEPTH ? k0 * ld : k0));
+    if (k0 + kDepth <= end) {
 #pragma unroll
-    for (int i = 0; i < kLoads; ++i) {
-      if (k0 + kDepth <= end) dma16(at, off[i], lds + (uint32_t)i * 1024u);
-      else dma16_from(k0 + depth_of(i) < end ? (const char*)at + off[i] : (const char*)g_zero_words, lds + (uint32_t)i * 1024u);
+      for (int i = 0; i < kLoads; ++i) dma16(at, off[i], lds + (uint32_t)i * 1024u);
+    } else {
+#pragma unroll
+      for (int i = 0; i < kLoads; ++i)
+        dma16_from(k0 + depth_of(i) < end ? (const char*)at + off[i] : (const char*)g_zero_words, lds + (uint32_t)i * 1024u);
     }
   }
   __device__ __forceinline__ bf16x8 read(const char* panel, int s) const {
