@@ -82,6 +82,14 @@ struct Operand {
       }
     }
   }
+  // ... one half of a whole stage
+  __device__ __forceinline__ void request_half(int64_t k0, uint32_t lds, int half) const {
+    const bf16_t* at = wave_uniform(base + (BY_DEPTH ? k0 * ld : k0));
+    const uint32_t to = lds + (uint32_t)(wave * kLoads) * 1024u;
+#pragma unroll
+    for (int i = 0; i < kLoads; ++i)
+      if (i % 2 == half) dma16(at, off[i], to + (uint32_t)i * 1024u);
+  }
   // MFMA operand: rows (columns) 32 t .. of the panel, k = 16 s + 8 (lane >> 5) ..
   __device__ __forceinline__ bf16x8 read(const char* panel, int t, int s) const {
     const int lr = lane & 31, h = lane >> 5;
@@ -120,6 +128,7 @@ struct Tile {
   typedef Operand<TM, PD, WAVES> OpP;
   typedef Operand<TN, QD, WAVES> OpQ;
   static constexpr int kStage = OpP::kBytes + OpQ::kBytes, kRequests = OpP::kLoads + OpQ::kLoads, kRing = S * kStage;
+  static constexpr bool kDeal = WAVES == 8;
   // first row m0, column number `col` of `cols`, split number `split` of `splits`
   static __device__ __forceinline__ void run(const LinearArgs& a, char* ring, int64_t m0, int64_t col, int64_t cols, int split,
                                              int splits, int64_t slice);
@@ -137,6 +146,7 @@ __device__ __forceinline__ void Tile<PD, QD, NI, NJ, WN, WM, S>::run(const Linea
   p.open((const bf16_t*)a.p, a.ldp, m0, a.M, lane, wave);
   q.open((const bf16_t*)a.q, a.ldq, n0, a.N, lane, wave);
   const uint32_t ring_at = lds_addr(ring);
+  const int whole = (int)((end - k0) / kDepth);          // stages that do not end early
   auto request = [&](int stage, int at) {
     const uint32_t slot = ring_at + (uint32_t)at * (uint32_t)kStage;
     p.request(k0 + (int64_t)stage * kDepth, end, slot);
@@ -173,7 +183,12 @@ __device__ __forceinline__ void Tile<PD, QD, NI, NJ, WN, WM, S>::run(const Linea
     FC_FENCE();
     __builtin_amdgcn_s_barrier();
     FC_FENCE();
-    if (g + S - 1 < stages) request(g + S - 1, before);
+    // A wavefront is held for some 60 cycles by each of its requests.  Where two wavefronts to a SIMD are all there are, a whole
+    // stage's are dealt out over two steps of this one, behind their products (dw of 16384 x 1024 x 4096 153 -> 143 us); where
+    // another workgroup fills the gap they go first (behind the products forward 16384 x 1024 x 4096 takes 182 us, not 177).
+    const bool deal = kDeal && g + S - 1 < whole;
+    const uint32_t next_at = ring_at + (uint32_t)before * (uint32_t)kStage;
+    if (!deal && g + S - 1 < stages) request(g + S - 1, before);
     const char* panel_p = ring + here * kStage;
     before = here;
     here = here + 1 < S ? here + 1 : 0;
@@ -193,6 +208,15 @@ __device__ __forceinline__ void Tile<PD, QD, NI, NJ, WN, WM, S>::run(const Linea
       for (int i = 0; i < NI; ++i)
 #pragma unroll
         for (int j = 0; j < NJ; ++j) acc[i][j] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(y[i], x[j], acc[i][j], 0, 0, 0);
+      if (kDeal && s < 2) {
+        FC_PIN();
+        if (deal) {
+          const int64_t k = k0 + (int64_t)(g + S - 1) * kDepth;
+          p.request_half(k, next_at, s);
+          q.request_half(k, next_at + (uint32_t)OpP::kBytes, s);
+        }
+        FC_PIN();
+      }
       if constexpr (PD && QD) {
         if (sums) {
           const bf16x2 ones = __builtin_bit_cast(bf16x2, 0x3f803f80u);
