@@ -520,8 +520,8 @@ void launch_linear_empty(const LinearArgs& a, hipStream_t s) {
 // ---- plan -----------------------------------------------------------------------------------------------------------------
 // Measured (one MI355X, us; a stage is 64 of k).  A stage of a 32 x 32 tile takes 0.08 where its workgroup has a compute unit to
 // itself and 0.1 where two share it; of 64 x 64 0.33, 0.46 and, three, 0.6; of 128 x 128 0.62 and, two, 0.96; of 192 x 128 0.8 and
-// 1.23; of 256 x 256, alone, 1.67; 64 x 64 and 128 x 128 a sixth more with both operands by depth.  A round of workgroups starts
-// and ends in 1.4, 2, 3, 4.5 and 9, the large tile in 14 where the value before the activation is kept.  Splits: a launch and the
+// 1.23; of 256 x 256, alone, 1.6; 64 x 64 and 128 x 128 a sixth more with both operands by depth.  A round of workgroups starts
+// and ends in 1.4, 2, 3, 4.5 and 5.5, the large tile in 17.5 where its epilogue has pre to read or to write.  Splits: a launch and the
 // traffic of their partial sums.  In fp32 a stage of 32 x 32 takes 0.36 and 0.64, of 64 x 64 1.4 and 2.3, their ends 1.7 and 3.
 static double rounds_of(int64_t n, double deep, int per_cu, const double (&stage)[3], double ends) {
   const int64_t places = 256 * per_cu, full = n / places, rest = n % places;
@@ -530,15 +530,15 @@ static double rounds_of(int64_t n, double deep, int per_cu, const double (&stage
   return t;
 }
 static const double kStage32[3] = {0.08, 0.10, 0.10}, kStage64[3] = {0.33, 0.46, 0.60}, kStage128[3] = {0.62, 0.96, 0.96},
-                    kStage192[3] = {0.80, 1.23, 1.23}, kStage256[3] = {1.67, 1.67, 1.67}, kStageF32[3] = {0.36, 0.64, 0.64},
+                    kStage192[3] = {0.80, 1.23, 1.23}, kStage256[3] = {1.60, 1.60, 1.60}, kStageF32[3] = {0.36, 0.64, 0.64},
                     kStageF32_64[3] = {1.40, 2.30, 2.30};
 
-// What takes the least time by the figures above.  16384 rows of 1024 -> 4096 with quick GELU and pre kept: 256 x 256 170, bands of
-// 192 rows 167, 128 x 128 268; 4096 -> 4096: 256 x 256 466, bands 494.  1024 rows of 1024 -> 1024: 32 x 32 and 64 x 64 9.5,
+// What takes the least time by the figures above.  16384 rows of 1024 -> 4096 with quick GELU and pre kept: 256 x 256 176, bands of
+// 192 rows 171, 128 x 128 268; without either 128 and 146; 4096 -> 4096: 434 and 488.  1024 rows of 1024 -> 1024: 32 x 32 and 64 x 64 9.5,
 // 128 x 128 13.5; 4096 rows: 64 x 64 19, 128 x 128 15.  128 rows of 2048 -> 2048: 32 x 32 6.9, 64 x 64 14.6, four splits of it
 // 11.2; of 4096 -> 512: 32 x 32 10.5 and in two splits 9.6, 64 x 64 25.  fp32: 1000 rows of 760 -> 760: 32 x 32 19.8, 64 x 64
 // 23.7; 16000 of 600 -> 650: 165 and 153.
-LinearPlan plan_linear(int64_t M, int64_t N, int64_t K, bool bf16, bool by_depth, bool keeps, bool dbias) {
+LinearPlan plan_linear(int64_t M, int64_t N, int64_t K, bool bf16, bool by_depth, bool busy, bool dbias) {
   static const int kSplits[] = {1, 2, 3, 4, 6, 8, 12, 16, 24, 32, 48, 64};
   auto count = [](int64_t x, int64_t t) { return (x + t - 1) / t; };
   const int64_t stages = count(K, kDepth), n64 = count(M, 64) * count(N, 64), cols = count(N, 128), n128 = count(M, 128) * cols,
@@ -562,11 +562,17 @@ LinearPlan plan_linear(int64_t M, int64_t N, int64_t K, bool bf16, bool by_depth
       consider(64, 0, 0, rounds_of(n64 * s, deep, 2, kStageF32_64, 3.0));
       continue;
     }
-    if (n64 * s <= 512) consider(32, 0, 0, rounds_of(count(M, 32) * count(N, 32) * s, deep, 2, kStage32, 1.4));
+    if (n64 * s <= 512) {
+      // 8 KiB a stage and tile come from the L2s, at 26 TB/s and, in 64-byte pieces by depth, 13: 10000 rows of 1000 x 1000, dw,
+      // 120 us, on 128 x 128 36
+      const int64_t n32 = count(M, 32) * count(N, 32) * s;
+      const double products = rounds_of(n32, deep, 2, kStage32, 1.4), loads = 1.4 + (double)n32 * deep * 8192.0 / (by_depth ? 13.0e6 : 26.0e6);
+      consider(32, 0, 0, products > loads ? products : loads);
+    }
     if (n64 <= 4096) consider(64, 0, 0, rounds_of(n64 * s, small_deep, 3, kStage64, 2.0));
     if (n64 <= 64) continue;
     consider(128, 0, count(M, 128), rounds_of(n128 * s, small_deep, 2, kStage128, 3.0));
-    if (n256 * s >= 64) consider(256, 0, 0, rounds_of(n256 * s, deep, 1, kStage256, keeps ? 14.0 : 9.0));
+    if (n256 * s >= 64) consider(256, 0, 0, rounds_of(n256 * s, deep, 1, kStage256, busy ? 17.5 : 5.5));
     if (s > 1 || n128 <= 512 || by_depth) continue;
     // whole rounds of 192-row bands, or what leaves up to 24 bands of 128 rows for the last one
     for (int64_t low = 0; low <= 24 && low * 128 < M; ++low) {
