@@ -2,10 +2,13 @@
 //
 //   m = b1 m + (1 - b1) g,  v = b2 v + (1 - b2) g^2,  p = p (1 - lr wd) - lr/(1 - b1^t) m / (sqrt(v / (1 - b2^t)) + eps)
 //
-// Bound by memory: 26 bytes an element with bf16 gradients (30 with fp32 moments written out and the bf16 copy), nothing is
-// used twice.  A workgroup takes a chunk of 4096 elements of one tensor, 16 a thread; all of a thread's loads are requested
+// Bound by memory: 28 bytes an element with bf16 gradients and a bf16 copy, 16 where the moments have 8 bits; nothing is used
+// twice.  A workgroup takes a chunk of 4096 elements of one tensor, 16 a thread; all of a thread's loads are requested
 // before the first is used.  The table says which chunk of which tensor a workgroup has, so that 180 small and large tensors
 // are one launch without a search.
+//
+// Measured on one MI355X, 151 million elements in 180 tensors, bf16 gradients and a bf16 copy: fp32 moments 788 us, 8-bit
+// moments 458 us, their values in fp32 140 us for each moment; all of them 5.3 to 5.4 TB/s, more than the 4.97 of a copy.
 #include "operators.hpp"
 
 namespace fc {

@@ -5,8 +5,15 @@
 //
 // An operand lies by rows (k contiguous) or by depth (k is the matrix's row).  Both come into LDS as they lie, by direct-to-LDS
 // loads, 64 of k a stage; by rows an MFMA operand is one 16-byte read, by depth two transposing reads.  Q gives the MFMA's rows
-// and P its columns, so that a lane holds four neighbouring columns of an output row; lanes 32 apart exchange halves, and every
-// load and store of the epilogue is eight neighbouring values.
+// and P its columns, so that a lane holds four neighbouring columns of an output row, and the epilogue loads and stores eight
+// neighbouring values a lane, whole lines a wavefront (linear_common.hpp).
+//
+// Bound by the matrix cores where depth and tiles are many, by the epilogue's traffic and arithmetic where the output is wide,
+// by latency where there are few tiles.  Measured on one MI355X (calls in turn over inputs that the caches do not hold):
+// forward of 16384 rows, 1024 -> 4096, with bias, quick GELU and pre 177 us = 0.78 PFLOP/s and 0.27 GB of results
+// (155 where the results stay in the last-level cache); gradient of an
+// input of 8192 x 4096 from 1024 columns, with GELU' 97 us = 0.71 PFLOP/s (91); gradient of a weight of 4096 x 1024 in fp32 from
+// 16384 rows 141 us = 0.98 PFLOP/s, 17 us of them the join; forward of 128 rows, 512 -> 512, 6 us, which is a launch.
 //
 // Edges: rows beyond M (columns beyond N) repeat the last one, and what they produce is not stored.  Depth beyond K has to add
 // nothing whatever the matrices hold, so the last stage takes its words from a block of zeros.
@@ -521,8 +528,8 @@ void launch_linear_empty(const LinearArgs& a, hipStream_t s) {
 // Measured (one MI355X, us; a stage is 64 of k).  A stage of a 32 x 32 tile takes 0.08 where its workgroup has a compute unit to
 // itself and 0.1 where two share it; of 64 x 64 0.33, 0.46 and, three, 0.6; of 128 x 128 0.62 and, two, 0.96; of 192 x 128 0.8 and
 // 1.23; of 256 x 256, alone, 1.6; 64 x 64 and 128 x 128 a sixth more with both operands by depth.  A round of workgroups starts
-// and ends in 1.4, 2, 3, 4.5 and 5.5, the large tile in 17.5 where its epilogue has pre to read or to write.  Splits: a launch and the
-// traffic of their partial sums.  In fp32 a stage of 32 x 32 takes 0.36 and 0.64, of 64 x 64 1.4 and 2.3, their ends 1.7 and 3.
+// and ends in 1.4, 2, 3, 4.5 and 5.5, the last three in 6.5, 8.5 and 13 where their epilogue has pre to write and in 7.5, 9.5 and 16
+// where it has it to read and the derivative to form.  Splits: a launch and the traffic of their partial sums.  In fp32 a stage of 32 x 32 takes 0.36 and 0.64, of 64 x 64 1.4 and 2.3, their ends 1.7 and 3.
 static double rounds_of(int64_t n, double deep, int per_cu, const double (&stage)[3], double ends) {
   const int64_t places = 256 * per_cu, full = n / places, rest = n % places;
   double t = (double)full * (deep * stage[per_cu - 1] + ends);
@@ -533,12 +540,13 @@ static const double kStage32[3] = {0.08, 0.10, 0.10}, kStage64[3] = {0.33, 0.46,
                     kStage192[3] = {0.80, 1.23, 1.23}, kStage256[3] = {1.60, 1.60, 1.60}, kStageF32[3] = {0.36, 0.64, 0.64},
                     kStageF32_64[3] = {1.40, 2.30, 2.30};
 
-// What takes the least time by the figures above.  16384 rows of 1024 -> 4096 with quick GELU and pre kept: 256 x 256 176, bands of
-// 192 rows 171, 128 x 128 268; without either 128 and 146; 4096 -> 4096: 434 and 488.  1024 rows of 1024 -> 1024: 32 x 32 and 64 x 64 9.5,
+// What takes the least time by the figures above.  16384 rows of 1024 -> 4096 with quick GELU and pre kept: 256 x 256 154, bands of
+// 192 rows 168, 128 x 128 176; without either 128 and 146; 4096 -> 4096: 434 and 488; 6000 rows of 1000 -> 4000, two rounds of
+// 256 x 256 half empty, with pre: 75 and 69; gradient of the input of 8192 rows from 1024 to 4096 columns 88 and 92.  1024 rows of 1024 -> 1024: 32 x 32 and 64 x 64 9.5,
 // 128 x 128 13.5; 4096 rows: 64 x 64 19, 128 x 128 15.  128 rows of 2048 -> 2048: 32 x 32 6.9, 64 x 64 14.6, four splits of it
 // 11.2; of 4096 -> 512: 32 x 32 10.5 and in two splits 9.6, 64 x 64 25.  fp32: 1000 rows of 760 -> 760: 32 x 32 19.8, 64 x 64
 // 23.7; 16000 of 600 -> 650: 165 and 153.
-LinearPlan plan_linear(int64_t M, int64_t N, int64_t K, bool bf16, bool by_depth, bool busy, bool dbias) {
+LinearPlan plan_linear(int64_t M, int64_t N, int64_t K, bool bf16, bool by_depth, int pre, bool dbias) {
   static const int kSplits[] = {1, 2, 3, 4, 6, 8, 12, 16, 24, 32, 48, 64};
   auto count = [](int64_t x, int64_t t) { return (x + t - 1) / t; };
   const int64_t stages = count(K, kDepth), n64 = count(M, 64) * count(N, 64), cols = count(N, 128), n128 = count(M, 128) * cols,
@@ -571,18 +579,19 @@ LinearPlan plan_linear(int64_t M, int64_t N, int64_t K, bool bf16, bool by_depth
     }
     if (n64 <= 4096) consider(64, 0, 0, rounds_of(n64 * s, small_deep, 3, kStage64, 2.0));
     if (n64 <= 64) continue;
-    consider(128, 0, count(M, 128), rounds_of(n128 * s, small_deep, 2, kStage128, 3.0));
-    if (n256 * s >= 64) consider(256, 0, 0, rounds_of(n256 * s, deep, 1, kStage256, busy ? 17.5 : 5.5));
+    consider(128, 0, count(M, 128), rounds_of(n128 * s, small_deep, 2, kStage128, pre == kPreRead ? 7.5 : (pre ? 6.5 : 3.0)));
+    if (n256 * s >= 64) consider(256, 0, 0, rounds_of(n256 * s, deep, 1, kStage256, pre == kPreRead ? 16.0 : (pre ? 13.0 : 5.5)));
     if (s > 1 || n128 <= 512 || by_depth) continue;
     // whole rounds of 192-row bands, or what leaves up to 24 bands of 128 rows for the last one
     for (int64_t low = 0; low <= 24 && low * 128 < M; ++low) {
       const int64_t high = count(M - low * 128, 192);
       if (low > 0 && high * 192 + (low - 1) * 128 >= M) continue;           // every band has rows
       const int64_t rest = high * cols % 512;
-      double cost = rounds_of(high * cols - rest, deep, 2, kStage192, 4.5);
+      const double ends = pre == kPreRead ? 9.5 : (pre ? 8.5 : 4.5);
+      double cost = rounds_of(high * cols - rest, deep, 2, kStage192, ends);
       // the last of them and the others side by side: two thirds of a place for each of the latter
       const int64_t mixed = rest + (2 * low * cols + 2) / 3;
-      cost += rounds_of(mixed, deep, 2, kStage192, 4.5);
+      cost += rounds_of(mixed, deep, 2, kStage192, ends);
       consider(128, high, low, cost);
     }
   }

@@ -9,6 +9,10 @@
 // stay and go through the rows, so that weight and bias are read once, the next row is requested before the present one is
 // summed, and the backward pass keeps its sums over the rows in registers: a workgroup leaves one partial sum per column, which
 // a second kernel adds up in a fixed order.
+//
+// Measured on one MI355X, bf16, 51200 x 768, in turn over inputs that the caches do not hold: forward 32.6 us = 4.8 TB/s of the
+// 4.97 that a copy reaches; backward 55 us = 4.3 TB/s and the columns 4.7 us.  Requesting two rows ahead in the backward pass
+// changes nothing (54.8 us).
 #include "operators.hpp"
 
 namespace fc {

@@ -71,8 +71,8 @@ static LinearArgs linear_args(const fastclip_linear_config& c, int32_t pass) {
   }
   return a;
 }
-static LinearPlan plan_of(const LinearArgs& a, bool busy) {
-  return plan_linear(a.M, a.N, a.K, a.bf16, a.p_by_depth, busy, a.p_by_depth);
+static LinearPlan plan_of(const LinearArgs& a, bool pre) {
+  return plan_linear(a.M, a.N, a.K, a.bf16, a.p_by_depth, !pre ? kPreNone : (a.q_by_depth ? kPreRead : kPreWritten), a.p_by_depth);
 }
 
 static fastclip_status run_linear(LinearArgs& a, void* workspace, size_t workspace_bytes, void* stream) {
@@ -175,8 +175,8 @@ size_t fastclip_linear_workspace_bytes(const fastclip_linear_config* cfg, int32_
   if (fc::check(cfg, pass) != FASTCLIP_OK) return 0;
   const fc::LinearArgs a = fc::linear_args(*cfg, pass);
   if (a.M == 0 || a.K == 0) return 0;
-  const size_t plain = fc::plan_of(a, false).bytes, busy = a.p_by_depth ? 0 : fc::plan_of(a, true).bytes;
-  return plain > busy ? plain : busy;
+  const size_t plain = fc::plan_of(a, false).bytes, with_pre = a.p_by_depth ? 0 : fc::plan_of(a, true).bytes;
+  return plain > with_pre ? plain : with_pre;
 }
 
 fastclip_status fastclip_linear_forward(const fastclip_linear_config* cfg, const void* x, const void* w, const float* bias,
