@@ -11,8 +11,8 @@
 // a second kernel adds up in a fixed order.
 //
 // Measured on one MI355X, bf16, 51200 x 768, in turn over inputs that the caches do not hold: forward 32.6 us = 4.8 TB/s of the
-// 4.97 that a copy reaches; backward 55 us = 4.3 TB/s and the columns 4.7 us.  Requesting two rows ahead in the backward pass
-// changes nothing (54.8 us).
+// 4.97 that a copy reaches; backward 47 us = 5.0 TB/s and the columns, 4.5 us.  Requesting two rows ahead in the backward pass
+// changes nothing.
 #include "operators.hpp"
 
 namespace fc {
@@ -373,8 +373,12 @@ __global__ void __launch_bounds__(1024) k_layer_norm_columns(const float* partia
 
 constexpr int64_t kNormWave = 1024, kNormGroup = 4096;     // longest row of a wavefront and of a workgroup
 
-int layer_norm_groups(int64_t rows, int64_t d) {
-  const int64_t per = d <= kNormWave ? 4 : 1, most = d <= kNormWave ? 1024 : (d <= kNormGroup ? 512 : 256);
+// Two workgroups a compute unit have enough in flight, and more of them that read two streams and write one are slower: 51200 rows of
+// 768 in bf16 50.8 us with 512, 51.2 with 768, 59.1 with 1024, 78 with 256; in fp32, 30000 rows, 57.0, 59.7, 63.3, 58.3; 8192 of
+// 4096 in bf16 53, 58, 64, 63.  Rows up to 512 in bf16 are one load a lane and want a third: 40000 of 512 29.4 with 768, 31.4 with 512.
+// Rows longer than registers hold are chains of short loads: 2000 of 6000 77 us with 1024, 116 with 512, 175 with 256.
+int layer_norm_groups(int64_t rows, int64_t d, bool x_bf16) {
+  const int64_t per = d <= kNormWave ? 4 : 1, most = d > kNormGroup ? 1024 : (d <= 512 && x_bf16 ? 768 : 512);
   const int64_t groups = (rows + per - 1) / per;
   return (int)(groups < most ? groups : most);
 }
@@ -423,7 +427,7 @@ void launch_layer_norm_forward(const NormArgs& a, hipStream_t s) {
 }
 
 void launch_layer_norm_backward(const NormArgs& a, float* dweight, float* dbias, hipStream_t s) {
-  const int groups = layer_norm_groups(a.rows, a.d);
+  const int groups = layer_norm_groups(a.rows, a.d, a.x_bf16);
   if (groups > 0) launch_types<true>(a, groups, s);
   if (dweight || dbias)
     hipLaunchKernelGGL(k_layer_norm_columns, dim3((unsigned)((2 * a.d + 31) / 32)), dim3(1024), 0, s, a.partial, groups, a.d,

@@ -20,7 +20,7 @@ struct NormArgs {
   float eps;
   bool x_bf16, y_bf16;
 };
-int layer_norm_groups(int64_t rows, int64_t d);     // workgroups of the backward pass = partial sums per column
+int layer_norm_groups(int64_t rows, int64_t d, bool x_bf16);     // workgroups of the backward pass = partial sums per column
 void launch_layer_norm_forward(const NormArgs& a, hipStream_t s);
 void launch_layer_norm_backward(const NormArgs& a, float* dweight, float* dbias, hipStream_t s);
 

@@ -146,7 +146,7 @@ fastclip_status fastclip_layer_norm_forward(const fastclip_layer_norm_config* cf
 
 size_t fastclip_layer_norm_backward_workspace_bytes(const fastclip_layer_norm_config* cfg) {
   if (fc::check(cfg) != FASTCLIP_OK) return 0;
-  const int groups = fc::layer_norm_groups(cfg->rows, cfg->d);
+  const int groups = fc::layer_norm_groups(cfg->rows, cfg->d, cfg->x_dtype == FASTCLIP_BF16);
   return fc::round_up(sizeof(float) * 2 * (size_t)cfg->d * (size_t)(groups > 0 ? groups : 1), 256);
 }
 
