@@ -529,7 +529,9 @@ void launch_linear_empty(const LinearArgs& a, hipStream_t s) {
 // itself and 0.1 where two share it; of 64 x 64 0.33, 0.46 and, three, 0.6; of 128 x 128 0.62 and, two, 0.96; of 192 x 128 0.8 and
 // 1.23; of 256 x 256, alone, 1.6; 64 x 64 and 128 x 128 a sixth more with both operands by depth.  A round of workgroups starts
 // and ends in 1.4, 2, 3, 4.5 and 5.5, the last three in 6.5, 8.5 and 13 where their epilogue has pre to write and in 7.5, 9.5 and 16
-// where it has it to read and the derivative to form.  Splits: a launch and the traffic of their partial sums.  In fp32 a stage of 32 x 32 takes 0.36 and 0.64, of 64 x 64 1.4 and 2.3, their ends 1.7 and 3.
+// where it has it to read and the derivative to form.  Splits: a launch and the traffic of their partial sums.
+// In fp32 a stage of 32 x 32 takes 0.36, 0.64 and, three with 16-byte loads and not both operands by depth, 0.84, of 64 x 64 1.4 and
+// 2.3, their ends 1.7 and 3, 5 beside the three.
 static double rounds_of(int64_t n, double deep, int per_cu, const double (&stage)[3], double ends) {
   const int64_t places = 256 * per_cu, full = n / places, rest = n % places;
   double t = (double)full * (deep * stage[per_cu - 1] + ends);
@@ -537,16 +539,16 @@ static double rounds_of(int64_t n, double deep, int per_cu, const double (&stage
   return t;
 }
 static const double kStage32[3] = {0.08, 0.10, 0.10}, kStage64[3] = {0.33, 0.46, 0.60}, kStage128[3] = {0.62, 0.96, 0.96},
-                    kStage192[3] = {0.80, 1.23, 1.23}, kStage256[3] = {1.60, 1.60, 1.60}, kStageF32[3] = {0.36, 0.64, 0.64},
+                    kStage192[3] = {0.80, 1.23, 1.23}, kStage256[3] = {1.60, 1.60, 1.60}, kStageF32[3] = {0.36, 0.64, 0.84},
                     kStageF32_64[3] = {1.40, 2.30, 2.30};
 
 // What takes the least time by the figures above.  16384 rows of 1024 -> 4096 with quick GELU and pre kept: 256 x 256 154, bands of
 // 192 rows 168, 128 x 128 176; without either 128 and 146; 4096 -> 4096: 434 and 488; 6000 rows of 1000 -> 4000, two rounds of
 // 256 x 256 half empty, with pre: 75 and 69; gradient of the input of 8192 rows from 1024 to 4096 columns 88 and 92.  1024 rows of 1024 -> 1024: 32 x 32 and 64 x 64 9.5,
 // 128 x 128 13.5; 4096 rows: 64 x 64 19, 128 x 128 15.  128 rows of 2048 -> 2048: 32 x 32 6.9, 64 x 64 14.6, four splits of it
-// 11.2; of 4096 -> 512: 32 x 32 10.5 and in two splits 9.6, 64 x 64 25.  fp32: 1000 rows of 760 -> 760: 32 x 32 19.8, 64 x 64
-// 23.7; 16000 of 600 -> 650: 165 and 153.
-LinearPlan plan_linear(int64_t M, int64_t N, int64_t K, bool bf16, bool by_depth, int pre, bool dbias) {
+// 11.2; of 4096 -> 512: 32 x 32 10.5 and in two splits 9.6, 64 x 64 25.  fp32: 1000 rows of 760 -> 760: 32 x 32 15.7, 64 x 64
+// 23.8; 16000 of 600 -> 650: 136 and 153, its input's gradient, in words of 4 bytes, 199 and 160.
+LinearPlan plan_linear(int64_t M, int64_t N, int64_t K, bool bf16, bool by_depth, int pre, bool dbias, bool wide) {
   static const int kSplits[] = {1, 2, 3, 4, 6, 8, 12, 16, 24, 32, 48, 64};
   auto count = [](int64_t x, int64_t t) { return (x + t - 1) / t; };
   const int64_t stages = count(K, kDepth), n64 = count(M, 64) * count(N, 64), cols = count(N, 128), n128 = count(M, 128) * cols,
@@ -566,8 +568,9 @@ LinearPlan plan_linear(int64_t M, int64_t N, int64_t K, bool bf16, bool by_depth
       best.tile = tile; best.high = (int)high; best.low = (int)low; best.splits = s; best.slice = slice * kDepth;
     };
     if (!bf16) {
-      consider(32, 0, 0, rounds_of(count(M, 32) * count(N, 32) * s, deep, 2, kStageF32, 1.7));
-      consider(64, 0, 0, rounds_of(n64 * s, deep, 2, kStageF32_64, 3.0));
+      const bool three = wide && !by_depth;
+      consider(32, 0, 0, rounds_of(count(M, 32) * count(N, 32) * s, deep, three ? 3 : 2, kStageF32, 1.7));
+      consider(64, 0, 0, rounds_of(n64 * s, deep, 2, kStageF32_64, three ? 5.0 : 3.0));
       continue;
     }
     if (n64 * s <= 512) {

@@ -16,8 +16,8 @@
 // Edges: rows beyond M (columns beyond N) repeat the last one, and what they produce is not stored; depth beyond K comes from a
 // block of zeros.
 //
-// Measured on one MI355X: 1000 rows, 760 -> 760, forward with a residual 21 us, 55 TFLOP/s; a product of its size would take 8 us at
-// the 139 TFLOP/s of a large one, but is 768 tiles of 32 x 32 over 1024 SIMDs, each a chain of 24 blocks of 1024 cycles.
+// Measured on one MI355X: 1000 rows, 760 -> 760, forward with a residual 17 us, 68 TFLOP/s; the matrix cores alone would take 8 us
+// for its 768 tiles, three a compute unit, and each of their wavefronts waits for its six blocks one after another.
 #include "linear_common.hpp"
 
 namespace fc {
@@ -114,7 +114,13 @@ __global__ void __launch_bounds__(256) k_linear_f32(LinearArgs a, uint32_t rows,
   typedef Operand32<QD, WIDE> OpQ;
   constexpr uint32_t kBuffer = 2 * kPanel32;
   constexpr int kRequests = OpP::kLoads + OpQ::kLoads;
-  __shared__ __attribute__((aligned(1024))) char ring[4 * 2 * kBuffer];      // per wavefront two blocks; then the parts of the sums
+  // Per wavefront the blocks on their way, then the parts of the sums.  A shared tile's wavefront has one: a block is in registers
+  // before the next takes its place, and four workgroups instead of two share a compute unit and cover the wait (1000 rows of 760
+  // -> 760 19.6 -> 15.7 us).  Requests of single words hold registers for two only, and want two blocks (a weight's gradient of 650 x
+  // 600 from 8000 rows 84 us, 91 with one).
+  constexpr bool kOne = SHARED && WIDE;
+  constexpr int kBuffers = kOne ? 1 : 2;
+  __shared__ __attribute__((aligned(1024))) char ring[4 * kBuffers * kBuffer];
   const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6), lr = lane & 31, hk = lane >> 5;
   const TilePlace place = tile_place(blockIdx.x, gridDim.x, rows, cols);
   const int64_t m0 = SHARED ? place.m * 32 : place.m * 64 + 32 * (wave & 1), n0 = SHARED ? place.n * 32 : place.n * 64 + 32 * (wave >> 1);
@@ -133,7 +139,7 @@ __global__ void __launch_bounds__(256) k_linear_f32(LinearArgs a, uint32_t rows,
   float total = 0.f;
 
   constexpr int64_t kStep = (SHARED ? 4 : 1) * kBlock32;
-  const char* mine = ring + wave * 2 * kBuffer;
+  const char* mine = ring + wave * kBuffers * kBuffer;
   const uint32_t mine_at = lds_addr(mine);
   auto request = [&](int64_t k, uint32_t buffer) {
     p.request(k, end, mine_at + buffer);
@@ -143,7 +149,7 @@ __global__ void __launch_bounds__(256) k_linear_f32(LinearArgs a, uint32_t rows,
   const int64_t first = k0 + (SHARED ? wave * kBlock32 : 0);
   if (first < end) request(first, 0);
   for (int64_t k = first; k < end; k += kStep) {
-    if (k + kStep < end) {
+    if (!kOne && k + kStep < end) {
       request(k + kStep, here ^ kBuffer);
       wait_vmcnt<kRequests>();                   // the older block's have landed
     } else {
@@ -154,6 +160,14 @@ __global__ void __launch_bounds__(256) k_linear_f32(LinearArgs a, uint32_t rows,
     Words32 x, y;
     OpP::read(x, mine + here, lr, hk);
     OpQ::read(y, mine + here + kPanel32, lr, hk);
+    if constexpr (kOne) {                        // the block is in registers: the next takes its place
+      FC_FENCE();
+      __builtin_amdgcn_s_waitcnt(0xc07f);        // lgkmcnt 0
+      __builtin_amdgcn_wave_barrier();
+      FC_FENCE();
+      if (k + kStep < end) request(k + kStep, 0);
+      FC_FENCE();
+    }
 #pragma unroll
     for (int s = 0; s < 4; ++s)
 #pragma unroll
@@ -166,9 +180,11 @@ __global__ void __launch_bounds__(256) k_linear_f32(LinearArgs a, uint32_t rows,
         total += some;
       }
     }
-    FC_FENCE();                                  // the block's reads are over before the next request takes its place
-    __builtin_amdgcn_wave_barrier();
-    here ^= kBuffer;
+    if constexpr (!kOne) {
+      FC_FENCE();                                // the block's reads are over before the next request takes its place
+      __builtin_amdgcn_wave_barrier();
+      here ^= kBuffer;
+    }
   }
 
   float* bias_to = splits > 1 ? a.partial + (int64_t)splits * a.M * a.N + (int64_t)place.split * a.M : a.dbias;

@@ -55,9 +55,10 @@ struct LinearPlan {
   int bias_parts;          // partial sums of dbias, with splits
   size_t bytes;            // workspace
 };
-// by_depth: both operands are; pre: what the epilogue does with it; dbias: room for its partial sums
+// by_depth: both operands are; pre: what the epilogue does with it; dbias: room for its partial sums; wide (fp32): sizes and strides
+// are whole 16-byte words
 enum { kPreNone = 0, kPreWritten = 1, kPreRead = 2 };
-LinearPlan plan_linear(int64_t M, int64_t N, int64_t K, bool bf16, bool by_depth, int pre, bool dbias);
+LinearPlan plan_linear(int64_t M, int64_t N, int64_t K, bool bf16, bool by_depth, int pre, bool dbias, bool wide = true);
 void launch_linear_bf16(const LinearArgs& a, const LinearPlan& plan, hipStream_t s);
 void launch_linear_f32(const LinearArgs& a, const LinearPlan& plan, hipStream_t s);
 void launch_linear_join(const LinearArgs& a, const LinearPlan& plan, hipStream_t s);   // sums of the splits' partial results

@@ -72,7 +72,9 @@ static LinearArgs linear_args(const fastclip_linear_config& c, int32_t pass) {
   return a;
 }
 static LinearPlan plan_of(const LinearArgs& a, bool pre) {
-  return plan_linear(a.M, a.N, a.K, a.bf16, a.p_by_depth, !pre ? kPreNone : (a.q_by_depth ? kPreRead : kPreWritten), a.p_by_depth);
+  const int64_t words = a.ldp | a.ldq | (a.p_by_depth ? a.M : a.K) | (a.q_by_depth ? a.N : a.K);
+  return plan_linear(a.M, a.N, a.K, a.bf16, a.p_by_depth, !pre ? kPreNone : (a.q_by_depth ? kPreRead : kPreWritten), a.p_by_depth,
+                     words % 4 == 0);
 }
 
 static fastclip_status run_linear(LinearArgs& a, void* workspace, size_t workspace_bytes, void* stream) {
